@@ -276,6 +276,82 @@ int et_select_stats(int32_t n, const double* importance, const uint64_t* t_dw_ns
 int et_train_step(et_ctx* ctx, const void* x_dev, const int32_t* y_dev, const uint8_t* mask_host /*[N]*/,
                   const et_opt* opt, float* loss_host);
 
+/* ---- Losses of log probabilities, and what is done to many gradients at once: stand-alone operators.
+ * Like et_importance_reduce_static they take device pointers and host descriptors that are read before the call returns,
+ * enqueue a few kernels on `hip_stream` (NULL = the default stream of the current device) on that stream's device, allocate nothing,
+ * copy nothing from or to host memory and do not wait, so that a call may be captured into a graph.  Their scratch is
+ * `workspace_dev`: 16-byte aligned, at least the bytes that the function beside each states (which depend on the sizes alone), in
+ * any state; a call leaves nothing in it that a later one reads.  Calls (and replays of captured ones) that share a workspace must not overlap.
+ * Sums run in a fixed order: a call on the same inputs gives the same bits.  ET_ENOMEM: the workspace is too small.
+ *
+ * Logits: row r of `classes` values starts at logits_dev + r * row_stride (in elements, row_stride >= classes), of type `dtype` (ET_F32 |
+ * ET_BF16).  The gradient has the same shape, a stride and a type of its own; grad_dev == NULL: no gradient is computed.  It may be logits_dev itself
+ * (same stride and type), and must not overlap the logits otherwise (ET_EINVAL).  Pointers need their element's alignment only.  Elements between the rows are
+ * neither read nor written.  label_dev[r] is the row's class (the action taken, the token produced); one outside [0, classes) masks the
+ * row: its logits and its other inputs are not used, whatever they hold, and its gradient is zero.  A logit of minus infinity has
+ * probability zero and gradient zero; a row with nothing but those has no distribution: it gives no loss and a gradient of zero, but counts among the unmasked.
+ * Softmax statistics are held in float32, a row's log probability and everything that is derived from it per row, and the sums over rows in float64;
+ * gradients are rounded once. */
+
+/* Clipped policy loss with a term for the divergence from a reference, and its gradient.  Per unmasked row, with p the softmax of its logits, lp = log p[label],
+ * ratio = exp(lp - old_logp) and A = advantage:
+ *   clipped   = (A > 0 and ratio > 1 + clip_high) or (A < 0 and ratio < 1 - clip_low)
+ *   surrogate = A * (clipped ? that border : ratio)        (the smaller of the clipped and the unclipped product)
+ *   kl        = exp(d) - d - 1, d = ref_logp - lp          if ref_logp_dev is given: an estimate from the label alone, never negative
+ *             = sum_j p[j] (log p[j] - log q[j])           if ref_logits_dev is: exactly, q their softmax
+ *             = 0                                          if neither is (both: ET_EINVAL)
+ *   loss      = sum over unmasked rows of weight * (kl_coef * kl - surrogate);  weight_dev == NULL: 1 / (number of unmasked rows)
+ * The gradient is that of `loss`; old_logp, advantage, the reference and the weights are constants, and a clipped row's surrogate has none.
+ * No unmasked row: loss 0. */
+typedef struct {
+  const float* old_logp_dev;    /* [rows] log probability of the label when it was drawn */
+  const float* advantage_dev;   /* [rows] */
+  const float* ref_logp_dev;    /* [rows] or NULL */
+  const void* ref_logits_dev;   /* the reference's logits, of the logits' type, or NULL */
+  int64_t ref_stride;           /* elements from one row of them to the next, >= classes */
+  const float* weight_dev;      /* [rows] or NULL */
+  float clip_low, clip_high;    /* >= 0, clip_low <= 1 */
+  float kl_coef;                /* finite */
+  float* logp_dev;              /* out, [rows] or NULL: lp; 0 of a masked row, minus infinity of one without a distribution */
+  float* stats_dev;             /* out, [3] or NULL: the sums of weight * surrogate, weight * kl and weight * clipped */
+} et_policy;
+size_t et_policy_loss_ws_bytes(int32_t rows);
+int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_t dtype, int64_t row_stride, const int32_t* label_dev,
+                   const et_policy* policy, void* grad_dev, int32_t grad_dtype, int64_t grad_stride, void* workspace_dev,
+                   size_t workspace_bytes, void* hip_stream, float* loss_dev);
+
+/* Preference loss of pairs of sequences, and its gradient.  Sequence i is the rows offsets[i] .. offsets[i+1] - 1; sequence 2p is the preferred
+ * one of pair p, 2p + 1 the other.  With L[i] the sum of its unmasked rows' log probabilities of their labels (0 of an empty sequence):
+ *   z = beta * ((L[2p] - ref[2p]) - (L[2p+1] - ref[2p+1]))
+ *   loss = mean over pairs of -(1 - label_smoothing) log sigmoid(z) - label_smoothing log sigmoid(-z)
+ * Rows in front of the first sequence and behind the last are neither read nor written.  Offsets that descend or leave [0, rows]
+ * are cut to where they do not. */
+typedef struct {
+  const int32_t* offsets_dev;   /* [2 pairs + 1], ascending; NULL: every row is a sequence (rows = 2 pairs) */
+  const float* ref_logp_dev;    /* [2 pairs] the reference's sums; NULL: zeros */
+  float beta;                   /* > 0 */
+  float label_smoothing;        /* in [0, 1] */
+  float* logp_dev;              /* out, [2 pairs] or NULL: L */
+  float* stats_dev;             /* out, [2] or NULL: the mean of z, the share of pairs with z > 0 */
+} et_preference;
+size_t et_preference_loss_ws_bytes(int32_t rows, int32_t pairs);
+int et_preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void* logits_dev, int32_t dtype, int64_t row_stride,
+                       const int32_t* label_dev, const et_preference* preference, void* grad_dev, int32_t grad_dtype, int64_t grad_stride,
+                       void* workspace_dev, size_t workspace_bytes, void* hip_stream, float* loss_dev);
+
+/* Euclidean norm of n gradients as one vector, and (tensor_norm_dev [n], or NULL) of each.  grad_dev and numel are host arrays; tensors are
+ * contiguous, of type `dtype`, aligned to their element; numel[i] = 0 is allowed (the pointer is not used then), n = 0 too (norm 0).
+ * Squares are added in float64: no overflow or underflow inside. */
+size_t et_grad_norm_ws_bytes(int32_t n, const uint64_t* numel);
+int et_grad_norm(int32_t n, const void* const* grad_dev, const uint64_t* numel, int32_t dtype, void* workspace_dev, size_t workspace_bytes,
+                 void* hip_stream, float* norm_dev, float* tensor_norm_dev);
+
+/* The same, and clipping: out[i] = grad[i] * c, c = max_norm / norm if norm > max_norm, else 1, rounded to float32 once.  A norm that is not finite leaves
+ * the values as they are: the caller sees it in norm_dev.  out_dev == NULL or out_dev[i] == grad_dev[i]: in place (nothing is written where c = 1); otherwise
+ * out[i] must not overlap any gradient.  max_norm >= 0.  Workspace: et_grad_norm_ws_bytes. */
+int et_grad_clip(int32_t n, const void* const* grad_dev, void* const* out_dev, const uint64_t* numel, int32_t dtype, float max_norm,
+                 void* workspace_dev, size_t workspace_bytes, void* hip_stream, float* norm_dev, float* tensor_norm_dev);
+
 /* Counters of the last et_train_step/et_importance call on this context: kernels launched in
  * the forward pass, in the backward pass and in the optimizer update. */
 int et_last_launch_counts(const et_ctx* ctx, int32_t* forward, int32_t* backward, int32_t* update);

@@ -36,6 +36,17 @@ class et_opt(C.Structure):
                 ("eps", C.c_float), ("momentum", C.c_float), ("wd", C.c_float), ("step", C.c_uint64)]
 
 
+class et_policy(C.Structure):
+    _fields_ = [("old_logp_dev", C.c_void_p), ("advantage_dev", C.c_void_p), ("ref_logp_dev", C.c_void_p), ("ref_logits_dev", C.c_void_p),
+                ("ref_stride", C.c_int64), ("weight_dev", C.c_void_p), ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl_coef", C.c_float),
+                ("logp_dev", C.c_void_p), ("stats_dev", C.c_void_p)]
+
+
+class et_preference(C.Structure):
+    _fields_ = [("offsets_dev", C.c_void_p), ("ref_logp_dev", C.c_void_p), ("beta", C.c_float), ("label_smoothing", C.c_float),
+                ("logp_dev", C.c_void_p), ("stats_dev", C.c_void_p)]
+
+
 class EtError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -63,6 +74,13 @@ def _load():
         "et_select": (C.c_int, [i32, C.POINTER(C.c_double), C.POINTER(u64), C.POINTER(u64), u64, C.c_uint32,
                                 C.c_uint32, C.POINTER(C.c_uint8), C.POINTER(u64)]),
         "et_train_step": (C.c_int, [vp, vp, vp, C.POINTER(C.c_uint8), C.POINTER(et_opt), C.POINTER(C.c_float)]),
+        "et_policy_loss_ws_bytes": (C.c_size_t, [i32]),
+        "et_policy_loss": (C.c_int, [i32, i32, vp, i32, C.c_int64, vp, C.POINTER(et_policy), vp, i32, C.c_int64, vp, C.c_size_t, vp, vp]),
+        "et_preference_loss_ws_bytes": (C.c_size_t, [i32, i32]),
+        "et_preference_loss": (C.c_int, [i32, i32, i32, vp, i32, C.c_int64, vp, C.POINTER(et_preference), vp, i32, C.c_int64, vp, C.c_size_t, vp, vp]),
+        "et_grad_norm_ws_bytes": (C.c_size_t, [i32, C.POINTER(u64)]),
+        "et_grad_norm": (C.c_int, [i32, C.POINTER(vp), C.POINTER(u64), i32, vp, C.c_size_t, vp, vp, vp]),
+        "et_grad_clip": (C.c_int, [i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(u64), i32, C.c_float, vp, C.c_size_t, vp, vp, vp]),
         "et_last_launch_counts": (C.c_int, [vp, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]),
         "et_kernel_timing": (C.c_int, [vp, i32]),
         "et_kernel_timing_read": (C.c_int, [vp, i32, C.POINTER(u64), C.POINTER(C.c_double), C.POINTER(C.c_double)]),
@@ -104,6 +122,7 @@ def _load():
 _lib = _load()
 EXPORTS = ["et_create", "et_destroy", "et_num_tensors", "et_tensor_info", "et_workspace_bytes", "et_workspace_min_bytes", "et_state_slots",
            "et_bind", "et_profile", "et_importance", "et_importance_master", "et_importance_reduce_static", "et_select", "et_select_stats", "et_tensor_metric", "et_train_step", "et_last_launch_counts",
+           "et_policy_loss", "et_policy_loss_ws_bytes", "et_preference_loss", "et_preference_loss_ws_bytes", "et_grad_norm", "et_grad_norm_ws_bytes", "et_grad_clip",
            "et_kernel_timing", "et_kernel_timing_read", "et_kernel_timing_overhead", "et_last_hip_error", "et_strerror", "et_debug_gemm_bf16", "et_debug_copy", "et_debug_mfma_peak", "et_debug_conv3x3",
            "et_debug_conv3x3_dw", "et_debug_depthwise3x3", "et_debug_depthwise3x3_ws_floats", "et_debug_affine_back", "et_debug_affine_back_ws_floats", "et_debug_flip3x3", "et_debug_dw_chunks", "et_debug_gemm_tile", "et_debug_gemm_bf16_act", "et_debug_conv3x3_plan", "et_debug_dw_group", "et_debug_conv_first",
            "et_debug_activation", "et_debug_conv3x3_split", "et_debug_attention", "et_debug_attention_long", "et_debug_attention_long_rest", "et_debug_gemm_bf16_colsum",
@@ -127,10 +146,22 @@ def _check(status, where, allow=(), ctx=None):
 
 
 def _ptr_array(ptrs):
+    if isinstance(ptrs, C.Array):
+        return ptrs
     arr = (C.c_void_p * len(ptrs))()
     for i, p in enumerate(ptrs):
         arr[i] = p
     return arr
+
+
+def pointers(ptrs):
+    """Device addresses as the host array that a call takes: made once by programs that pass the same tensors again and again."""
+    return _ptr_array(list(ptrs))
+
+
+def sizes(numel):
+    """Element counts, likewise."""
+    return numel if isinstance(numel, C.Array) else (C.c_uint64 * len(numel))(*[int(v) for v in numel])
 
 
 def make_desc(kind, dtype, batch, dims=(), tokens=0, patch_dim=0, width=0, heads=0, mlp=0, blocks=0, classes=0,
@@ -281,6 +312,49 @@ def et_train_step(ctx, x_dev, y_dev, mask, opt=None, want_loss=True):
                               C.byref(opt) if opt is not None else None, C.byref(loss) if want_loss else None),
            "et_train_step", ctx=ctx)
     return loss.value if want_loss else None
+
+
+def make_policy(old_logp, advantage, ref_logp=0, ref_logits=0, ref_stride=0, weight=0, clip_low=0.2, clip_high=0.2, kl_coef=0.0, logp=0, stats=0):
+    return et_policy(old_logp, advantage, ref_logp, ref_logits, ref_stride, weight, clip_low, clip_high, kl_coef, logp, stats)
+
+
+def et_policy_loss_ws_bytes(rows):
+    return _lib.et_policy_loss_ws_bytes(rows)
+
+
+def et_policy_loss(rows, classes, logits, dtype, row_stride, label, policy, grad, grad_dtype, grad_stride, ws, ws_bytes, stream, loss):
+    """Device addresses but for `policy` (make_policy); enqueues, waits for nothing."""
+    _check(_lib.et_policy_loss(rows, classes, logits, dtype, row_stride, label, C.byref(policy), grad, grad_dtype, grad_stride, ws, ws_bytes, stream, loss),
+           "et_policy_loss")
+
+
+def make_preference(offsets, ref_logp=0, beta=0.1, label_smoothing=0.0, logp=0, stats=0):
+    return et_preference(offsets, ref_logp, beta, label_smoothing, logp, stats)
+
+
+def et_preference_loss_ws_bytes(rows, pairs):
+    return _lib.et_preference_loss_ws_bytes(rows, pairs)
+
+
+def et_preference_loss(rows, pairs, classes, logits, dtype, row_stride, label, preference, grad, grad_dtype, grad_stride, ws, ws_bytes, stream, loss):
+    """Device addresses but for `preference` (make_preference); enqueues, waits for nothing."""
+    _check(_lib.et_preference_loss(rows, pairs, classes, logits, dtype, row_stride, label, C.byref(preference), grad, grad_dtype, grad_stride, ws, ws_bytes,
+                                   stream, loss), "et_preference_loss")
+
+
+def et_grad_norm_ws_bytes(numel):
+    return _lib.et_grad_norm_ws_bytes(len(numel), sizes(numel))
+
+
+def et_grad_norm(grad, numel, dtype, ws, ws_bytes, stream, norm, tensor_norm=0):
+    """grad, numel: lists, or what pointers() and sizes() made of them."""
+    _check(_lib.et_grad_norm(len(numel), _ptr_array(grad), sizes(numel), dtype, ws, ws_bytes, stream, norm, tensor_norm), "et_grad_norm")
+
+
+def et_grad_clip(grad, out, numel, dtype, max_norm, ws, ws_bytes, stream, norm, tensor_norm=0):
+    """out: like grad, or None to clip in place."""
+    _check(_lib.et_grad_clip(len(numel), _ptr_array(grad), _ptr_array(out) if out is not None else None, sizes(numel), dtype, max_norm, ws, ws_bytes, stream,
+                             norm, tensor_norm), "et_grad_clip")
 
 
 def et_last_launch_counts(ctx):

@@ -1,0 +1,43 @@
+// What the stand-alone operators of the C ABI check and set up in front of their launches.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "et.h"
+
+namespace et_op {
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline size_t type_size(int32_t dtype) { return dtype == ET_BF16 ? 2 : 4; }
+inline bool type_ok(int32_t dtype) { return dtype == ET_F32 || dtype == ET_BF16; }
+
+// The launches of a call go to the device of its stream, whichever device is current (kernels and device limits are looked up for the current one)
+struct OnDeviceOf {
+  int before = -1;
+  bool ok = true, switched = false;
+  int dev = -1;
+  explicit OnDeviceOf(hipStream_t s) {
+    ok = hipGetDevice(&before) == hipSuccess;
+    dev = before;
+    if (!ok || !s) return;
+    hipDevice_t d;
+    if (hipStreamGetDevice(s, &d) != hipSuccess) { ok = false; return; }
+    dev = (int)d;
+    if (dev != before) ok = switched = hipSetDevice(dev) == hipSuccess;
+  }
+  ~OnDeviceOf() {
+    if (switched) (void)hipSetDevice(before);
+  }
+};
+
+// bytes [begin, end) of a matrix of `rows` rows
+struct Span {
+  uintptr_t begin, end;
+  Span(const void* p, int64_t rows, int64_t cols, int64_t stride, size_t size)
+      : begin(reinterpret_cast<uintptr_t>(p)), end(begin + (size_t)((rows - 1) * stride + cols) * size) {}
+  bool meets(const Span& o) const { return begin < o.end && o.begin < end; }
+};
+
+}  // namespace et_op
