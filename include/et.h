@@ -346,11 +346,16 @@ size_t et_grad_norm_ws_bytes(int32_t n, const uint64_t* numel);
 int et_grad_norm(int32_t n, const void* const* grad_dev, const uint64_t* numel, int32_t dtype, void* workspace_dev, size_t workspace_bytes,
                  void* hip_stream, float* norm_dev, float* tensor_norm_dev);
 
-/* The same, and clipping: out[i] = grad[i] * c, c = max_norm / norm if norm > max_norm, else 1, rounded to float32 once.  A norm that is not finite leaves
- * the values as they are: the caller sees it in norm_dev.  out_dev == NULL or out_dev[i] == grad_dev[i]: in place (nothing is written where c = 1); otherwise
- * out[i] must not overlap any gradient.  max_norm >= 0.  Workspace: et_grad_norm_ws_bytes. */
+/* The same, and clipping: out[i] = grad[i] * c, c = max_norm / norm if norm > max_norm, else 1, with the norm and c each rounded to float32.  A norm that is not
+ * finite leaves the values as they are: the caller sees it in norm_dev.  out_dev == NULL or out_dev[i] == grad_dev[i]: in place (nothing is written where c = 1);
+ * otherwise out[i] must not overlap any gradient.  In place a tensor may be listed once only.  max_norm >= 0.  Workspace: et_grad_norm_ws_bytes. */
 int et_grad_clip(int32_t n, const void* const* grad_dev, void* const* out_dev, const uint64_t* numel, int32_t dtype, float max_norm,
                  void* workspace_dev, size_t workspace_bytes, void* hip_stream, float* norm_dev, float* tensor_norm_dev);
+
+/* The second half on its own, by a norm that lies in device memory: of other tensors than those that are scaled (an arena as one piece, a norm
+ * that was put together from several devices' or micro-batches' gradients). */
+int et_grad_scale(int32_t n, const void* const* grad_dev, void* const* out_dev, const uint64_t* numel, int32_t dtype, const float* norm_dev, float max_norm,
+                  void* hip_stream);
 
 /* Counters of the last et_train_step/et_importance call on this context: kernels launched in
  * the forward pass, in the backward pass and in the optimizer update. */

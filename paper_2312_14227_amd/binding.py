@@ -81,6 +81,7 @@ def _load():
         "et_grad_norm_ws_bytes": (C.c_size_t, [i32, C.POINTER(u64)]),
         "et_grad_norm": (C.c_int, [i32, C.POINTER(vp), C.POINTER(u64), i32, vp, C.c_size_t, vp, vp, vp]),
         "et_grad_clip": (C.c_int, [i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(u64), i32, C.c_float, vp, C.c_size_t, vp, vp, vp]),
+        "et_grad_scale": (C.c_int, [i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(u64), i32, vp, C.c_float, vp]),
         "et_last_launch_counts": (C.c_int, [vp, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]),
         "et_kernel_timing": (C.c_int, [vp, i32]),
         "et_kernel_timing_read": (C.c_int, [vp, i32, C.POINTER(u64), C.POINTER(C.c_double), C.POINTER(C.c_double)]),
@@ -122,7 +123,7 @@ def _load():
 _lib = _load()
 EXPORTS = ["et_create", "et_destroy", "et_num_tensors", "et_tensor_info", "et_workspace_bytes", "et_workspace_min_bytes", "et_state_slots",
            "et_bind", "et_profile", "et_importance", "et_importance_master", "et_importance_reduce_static", "et_select", "et_select_stats", "et_tensor_metric", "et_train_step", "et_last_launch_counts",
-           "et_policy_loss", "et_policy_loss_ws_bytes", "et_preference_loss", "et_preference_loss_ws_bytes", "et_grad_norm", "et_grad_norm_ws_bytes", "et_grad_clip",
+           "et_policy_loss", "et_policy_loss_ws_bytes", "et_preference_loss", "et_preference_loss_ws_bytes", "et_grad_norm", "et_grad_norm_ws_bytes", "et_grad_clip", "et_grad_scale",
            "et_kernel_timing", "et_kernel_timing_read", "et_kernel_timing_overhead", "et_last_hip_error", "et_strerror", "et_debug_gemm_bf16", "et_debug_copy", "et_debug_mfma_peak", "et_debug_conv3x3",
            "et_debug_conv3x3_dw", "et_debug_depthwise3x3", "et_debug_depthwise3x3_ws_floats", "et_debug_affine_back", "et_debug_affine_back_ws_floats", "et_debug_flip3x3", "et_debug_dw_chunks", "et_debug_gemm_tile", "et_debug_gemm_bf16_act", "et_debug_conv3x3_plan", "et_debug_dw_group", "et_debug_conv_first",
            "et_debug_activation", "et_debug_conv3x3_split", "et_debug_attention", "et_debug_attention_long", "et_debug_attention_long_rest", "et_debug_gemm_bf16_colsum",
@@ -355,6 +356,12 @@ def et_grad_clip(grad, out, numel, dtype, max_norm, ws, ws_bytes, stream, norm, 
     """out: like grad, or None to clip in place."""
     _check(_lib.et_grad_clip(len(numel), _ptr_array(grad), _ptr_array(out) if out is not None else None, sizes(numel), dtype, max_norm, ws, ws_bytes, stream,
                              norm, tensor_norm), "et_grad_clip")
+
+
+def et_grad_scale(grad, out, numel, dtype, norm, max_norm, stream):
+    """norm: the device address of one; out as in et_grad_clip."""
+    _check(_lib.et_grad_scale(len(numel), _ptr_array(grad), _ptr_array(out) if out is not None else None, sizes(numel), dtype, norm, max_norm, stream),
+           "et_grad_scale")
 
 
 def et_last_launch_counts(ctx):

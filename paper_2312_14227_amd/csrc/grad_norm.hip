@@ -72,22 +72,23 @@ __global__ __launch_bounds__(64) void tensor_kernel(Tensors t, const double* __r
   }
 }
 
-__global__ __launch_bounds__(256) void norm_kernel(const double* __restrict__ squares, int n, double max_norm, float* __restrict__ norm,
-                                                   float* __restrict__ scale) {
+__global__ __launch_bounds__(256) void norm_kernel(const double* __restrict__ squares, int n, float* __restrict__ norm) {
   __shared__ double red[4];
   double s = 0;
   for (int i = threadIdx.x; i < n; i += 256) s += squares[i];
-  s = sqrt(block_sum_d(s, red));
-  if (threadIdx.x != 0) return;
-  *norm = (float)s;
-  *scale = isfinite((float)s) && s > max_norm ? (float)(max_norm / s) : 1.f;
+  s = block_sum_d(s, red);
+  if (threadIdx.x == 0) *norm = (float)sqrt(s);
+}
+
+__device__ __forceinline__ float clip_scale(float norm, float max_norm) {
+  return isfinite(norm) && norm > max_norm ? (float)((double)max_norm / (double)norm) : 1.f;
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void scale_kernel(Tensors t, const float* __restrict__ scale) {
+__global__ __launch_bounds__(256) void scale_kernel(Tensors t, const float* __restrict__ norm, float max_norm) {
   const uint32_t c = t.begin[0] + blockIdx.x;
   const int k = tensor_of(t, c);
-  const float f = *scale;
+  const float f = clip_scale(*norm, max_norm);
   if (f == 1.f && t.out[k] == t.g[k]) return;
   const uint64_t off = (uint64_t)(c - t.begin[k]) * t.chunk;
   const T* g = (const T*)t.g[k] + off;
@@ -117,57 +118,78 @@ bool make_plan(int32_t n, const uint64_t* numel, Plan* p) {
   for (int32_t i = 0; i < n; i++) p->chunks += (numel[i] + p->chunk - 1) / p->chunk;
   return p->chunks < (1ull << 31);
 }
-size_t ws_bytes(int32_t n, const Plan& p) { return 256 + sizeof(double) * ((size_t)n + p.chunks); }
+size_t ws_bytes(int32_t n, const Plan& p) { return 64 + sizeof(double) * ((size_t)n + p.chunks); }
 
-int norm_and_clip(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, int32_t dtype, bool clip, float max_norm, void* ws,
-                  size_t bytes, void* hip_stream, float* norm, float* tensor_norm) {
-  if (n < 0 || (n > 0 && (!grad || !numel)) || !type_ok(dtype) || !ws || !norm || !aligned(ws, 16) || !aligned(norm, 4) || !aligned(tensor_norm, 4)) return ET_EINVAL;
-  if (clip && !(max_norm >= 0)) return ET_EINVAL;
+int check_tensors(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, int32_t dtype, const float* norm) {
+  if (n < 0 || (n > 0 && (!grad || !numel)) || !type_ok(dtype) || !norm || !aligned(norm, 4)) return ET_EINVAL;
   const size_t size = type_size(dtype);
   for (int32_t i = 0; i < n; i++) {
     if (numel[i] == 0) continue;
-    const void* o = clip && out ? out[i] : grad[i];
+    const void* o = out ? out[i] : grad[i];
     if (!grad[i] || !o || !aligned(grad[i], size) || !aligned(o, size) || numel[i] > (1ull << 48)) return ET_EINVAL;
     if (o != grad[i] && Span(grad[i], 1, (int64_t)numel[i], 0, size).meets(Span(o, 1, (int64_t)numel[i], 0, size))) return ET_EINVAL;
   }
+  return ET_OK;
+}
+
+// calls f(table, workgroups) for every launch over the chunks
+template <typename F>
+void each_batch(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, const Plan& p, F f) {
+  uint32_t next = 0;
+  for (int32_t i0 = 0; i0 < n; i0 += et::BATCH) {
+    et::Tensors t;
+    t.n = std::min<int32_t>(et::BATCH, n - i0);
+    t.first = i0;
+    t.chunk = p.chunk;
+    for (int k = 0; k < t.n; k++) {
+      t.begin[k] = next;
+      t.g[k] = grad[i0 + k];
+      t.out[k] = out ? out[i0 + k] : const_cast<void*>(grad[i0 + k]);
+      t.numel[k] = numel[i0 + k];
+      next += (uint32_t)((numel[i0 + k] + p.chunk - 1) / p.chunk);
+    }
+    t.begin[t.n] = next;
+    f(t, next - t.begin[0]);
+  }
+}
+
+void norm_launch(int32_t n, const void* const* grad, const uint64_t* numel, int32_t dtype, const Plan& p, void* ws, hipStream_t s, float* norm,
+                 float* tensor_norm) {
+  double* squares = (double*)ws;
+  double* part = squares + n;
+  each_batch(n, grad, nullptr, numel, p, [&](const et::Tensors& t, uint32_t grid) {
+    if (grid) {
+      if (dtype == ET_BF16) hipLaunchKernelGGL(et::squares_kernel<bf16>, dim3(grid), dim3(256), 0, s, t, part);
+      else hipLaunchKernelGGL(et::squares_kernel<float>, dim3(grid), dim3(256), 0, s, t, part);
+    }
+    hipLaunchKernelGGL(et::tensor_kernel, dim3(t.n), dim3(64), 0, s, t, part, squares, tensor_norm);
+  });
+  hipLaunchKernelGGL(et::norm_kernel, dim3(1), dim3(256), 0, s, squares, n, norm);
+}
+
+void scale_launch(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, int32_t dtype, const Plan& p, const float* norm, float max_norm,
+                  hipStream_t s) {
+  each_batch(n, grad, out, numel, p, [&](const et::Tensors& t, uint32_t grid) {
+    if (!grid) return;
+    if (dtype == ET_BF16) hipLaunchKernelGGL(et::scale_kernel<bf16>, dim3(grid), dim3(256), 0, s, t, norm, max_norm);
+    else hipLaunchKernelGGL(et::scale_kernel<float>, dim3(grid), dim3(256), 0, s, t, norm, max_norm);
+  });
+}
+
+// max_norm < 0: the norm only
+int norm_and_clip(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, int32_t dtype, float max_norm, void* ws, size_t bytes,
+                  void* hip_stream, float* norm, float* tensor_norm) {
+  const int rc = check_tensors(n, grad, out, numel, dtype, norm);
+  if (rc != ET_OK) return rc;
+  if (!ws || !aligned(ws, 16) || !aligned(tensor_norm, 4)) return ET_EINVAL;
   Plan p;
   if (!make_plan(n, numel, &p)) return ET_EINVAL;
   if (bytes < ws_bytes(n, p)) return ET_ENOMEM;
   const hipStream_t s = (hipStream_t)hip_stream;
   const OnDeviceOf on(s);
   if (!on.ok) return ET_EHIP;
-  float* scale = (float*)ws;
-  double* squares = (double*)ws + 32;
-  double* part = squares + n;
-  for (int pass = 0; pass < (clip ? 2 : 1); pass++) {
-    uint32_t next = 0;
-    for (int32_t i0 = 0; i0 < n; i0 += et::BATCH) {
-      et::Tensors t;
-      t.n = std::min<int32_t>(et::BATCH, n - i0);
-      t.first = i0;
-      t.chunk = p.chunk;
-      for (int k = 0; k < t.n; k++) {
-        t.begin[k] = next;
-        t.g[k] = grad[i0 + k];
-        t.out[k] = clip && out ? out[i0 + k] : const_cast<void*>(grad[i0 + k]);
-        t.numel[k] = numel[i0 + k];
-        next += (uint32_t)((numel[i0 + k] + p.chunk - 1) / p.chunk);
-      }
-      t.begin[t.n] = next;
-      const uint32_t grid = next - t.begin[0];
-      if (pass == 0) {
-        if (grid) {
-          if (dtype == ET_BF16) hipLaunchKernelGGL(et::squares_kernel<bf16>, dim3(grid), dim3(256), 0, s, t, part);
-          else hipLaunchKernelGGL(et::squares_kernel<float>, dim3(grid), dim3(256), 0, s, t, part);
-        }
-        hipLaunchKernelGGL(et::tensor_kernel, dim3(t.n), dim3(64), 0, s, t, part, squares, tensor_norm);
-      } else if (grid) {
-        if (dtype == ET_BF16) hipLaunchKernelGGL(et::scale_kernel<bf16>, dim3(grid), dim3(256), 0, s, t, scale);
-        else hipLaunchKernelGGL(et::scale_kernel<float>, dim3(grid), dim3(256), 0, s, t, scale);
-      }
-    }
-    if (pass == 0) hipLaunchKernelGGL(et::norm_kernel, dim3(1), dim3(256), 0, s, squares, n, (double)max_norm, norm, scale);
-  }
+  norm_launch(n, grad, numel, dtype, p, ws, s, norm, tensor_norm);
+  if (max_norm >= 0) scale_launch(n, grad, out, numel, dtype, p, norm, max_norm, s);
   return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
 }
 
@@ -182,12 +204,27 @@ size_t et_grad_norm_ws_bytes(int32_t n, const uint64_t* numel) {
 
 int et_grad_norm(int32_t n, const void* const* grad_dev, const uint64_t* numel, int32_t dtype, void* workspace_dev, size_t workspace_bytes,
                  void* hip_stream, float* norm_dev, float* tensor_norm_dev) {
-  return norm_and_clip(n, grad_dev, nullptr, numel, dtype, false, 0.f, workspace_dev, workspace_bytes, hip_stream, norm_dev, tensor_norm_dev);
+  return norm_and_clip(n, grad_dev, nullptr, numel, dtype, -1.f, workspace_dev, workspace_bytes, hip_stream, norm_dev, tensor_norm_dev);
 }
 
 int et_grad_clip(int32_t n, const void* const* grad_dev, void* const* out_dev, const uint64_t* numel, int32_t dtype, float max_norm,
                  void* workspace_dev, size_t workspace_bytes, void* hip_stream, float* norm_dev, float* tensor_norm_dev) {
-  return norm_and_clip(n, grad_dev, out_dev, numel, dtype, true, max_norm, workspace_dev, workspace_bytes, hip_stream, norm_dev, tensor_norm_dev);
+  if (!(max_norm >= 0)) return ET_EINVAL;
+  return norm_and_clip(n, grad_dev, out_dev, numel, dtype, max_norm, workspace_dev, workspace_bytes, hip_stream, norm_dev, tensor_norm_dev);
+}
+
+int et_grad_scale(int32_t n, const void* const* grad_dev, void* const* out_dev, const uint64_t* numel, int32_t dtype, const float* norm_dev, float max_norm,
+                  void* hip_stream) {
+  if (!(max_norm >= 0)) return ET_EINVAL;
+  const int rc = check_tensors(n, grad_dev, out_dev, numel, dtype, norm_dev);
+  if (rc != ET_OK) return rc;
+  Plan p;
+  if (!make_plan(n, numel, &p)) return ET_EINVAL;
+  const hipStream_t s = (hipStream_t)hip_stream;
+  const OnDeviceOf on(s);
+  if (!on.ok) return ET_EHIP;
+  scale_launch(n, grad_dev, out_dev, numel, dtype, p, norm_dev, max_norm, s);
+  return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
 }
 
 }  // extern "C"

@@ -211,3 +211,19 @@ def test_offsets_beyond_32_bits():
     et.et_grad_clip([g.data_ptr()], None, [n], et.ET_BF16, 6.5, ws.data_ptr(), room, torch.cuda.current_stream().cuda_stream, norm.data_ptr())
     torch.cuda.synchronize()
     assert norm.item() == 13.0 and [g[0].item(), g[-1].item(), g[n // 2].item()] == [1.5, 2.0, 6.0]
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("out", [None, 0, 3])
+@pytest.mark.parametrize("norm", [0.5, 2.0, float("inf"), float("nan")])
+def test_scaling_by_a_norm_from_elsewhere(norm, out, bf16):
+    import torch
+    from paper_2312_14227_amd import binding as et
+    c = Case([5000, 0, 70003, 1] + [9] * 130, bf16, out=out, gap=1)
+    given = torch.tensor([norm], device="cuda")
+    ptr = lambda vs: [v.data_ptr() if v.numel() else 0 for v in vs]  # noqa: E731
+    et.et_grad_scale(ptr(c.views), None if out is None else ptr(c.outs), c.sizes, et.ET_BF16 if bf16 else et.ET_F32, given.data_ptr(), 0.75,
+                     torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    f = 0.375 if norm == 2.0 else 1.0
+    assert all((np.abs(v.double().cpu().numpy() - f * h) <= (2.0 ** -8 if bf16 else 2.0 ** -24) * np.abs(h) * (f != 1)).all() for v, h in zip(c.outs, c.host))

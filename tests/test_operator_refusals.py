@@ -71,3 +71,12 @@ def test_grad_norm_and_clip_refuse(kw):
         with pytest.raises(et.EtError) as e:
             et.et_grad_norm(a["grad"], a["numel"], a["dtype"], a["ws"], room, 0, a["norm"], a["each"])
         assert e.value.status == et.ET_EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(grad=[A, 0]), dict(grad=[A, A + 2]), dict(dtype=2), dict(norm=0), dict(norm=A + 2), dict(numel=[8, 1 << 49]), dict(out=[A, 0]),
+                                dict(out=[A + 16, A]), dict(max_norm=-1.0), dict(max_norm=math.nan)])
+def test_grad_scale_refuses(kw):
+    a = dict(grad=[A, 2 * A], out=None, numel=[8, 8], dtype=et.ET_F32, max_norm=1.0, norm=A) | kw
+    with pytest.raises(et.EtError) as e:
+        et.et_grad_scale(a["grad"], a["out"], a["numel"], a["dtype"], a["norm"], a["max_norm"], 0)
+    assert e.value.status == et.ET_EINVAL
