@@ -305,9 +305,14 @@ def _bound(s):
         out = {"norm": norm[0], "tensor_norm": each}
         if s["op"] == "norm":
             return lambda: et.et_grad_norm(grads, numel, dtype, at(ws), ws.numel(), stream, at(norm), at(each)), out
-        outs = et.pointers([g.data_ptr() for g in s["outs"]])
+        # the arena is scaled as one piece, with what lies between its tensors
+        whole = et.pointers([at(s["arena"])]), et.pointers([at(s["out"])]), et.sizes([s["arena"].numel()])
         out["grads"] = s["out"]
-        return lambda: et.et_grad_clip(grads, outs, numel, dtype, s["max_norm"], at(ws), ws.numel(), stream, at(norm), at(each)), out
+
+        def clip():
+            et.et_grad_norm(grads, numel, dtype, at(ws), ws.numel(), stream, at(norm), at(each))
+            et.et_grad_scale(*whole, dtype, at(norm), s["max_norm"], stream)
+        return clip, out
     rows, C, ld, grad, loss = s["rows"], s["classes"], s["logits"].shape[1], s.get("grad"), f32(1)
     out = {"loss": loss[0]} | ({"grad": grad[:, :C]} if grad is not None else {})
     if s["op"] == "policy":
