@@ -32,6 +32,11 @@ struct OnDeviceOf {
   }
 };
 
+inline int device_cus(int dev) {
+  int n = 0;
+  return hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0 ? n : 256;
+}
+
 // bytes [begin, end) of a matrix of `rows` rows
 struct Span {
   uintptr_t begin, end;
