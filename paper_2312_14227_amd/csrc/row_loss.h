@@ -1,0 +1,725 @@
+// Kernels over rows of logits: softmax statistics, and the gradients of losses that depend on a row through the log probability of its label.
+//
+// Of a row they need a reference m near its maximum and S = sum exp(x - m), from which log p[a] = x[a] - m - log S.
+// The label's own term is left out of the sum, S = rest + its term: 1 - p[a] = rest / S, its gradient, and log p[a] = -log1p(rest / term) are exact to rounding also where
+// p[a] is close to 1.
+//
+// What bounds them: memory, with the vector units close behind.  An element costs a row's statistics some 8 issue slots, four of them the exponential, and the
+// gradient 8 more; a row of 128000 bf16 classes takes a compute unit 18 us of those and 24 us of its share of the memory.
+#pragma once
+#include <cmath>
+
+#include "context.h"
+#include "op_args.h"
+
+namespace et {
+namespace rows {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// Rows start at any element: vectors are loaded and stored at the alignment of an element, which global memory takes on this hardware
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// log2 e in float32 is LOG2E = (1 + SKEW) log2 e.  Exponentials taken with it are those of (1 + SKEW) (x - m), which moves log S by SKEW E[x - m]: of one sign, it adds up over the
+// rows of a sequence (the mean margin of 16 sequences of 500 rows was off by three times its other roundings), so it is taken off again, E from the first element of every vector
+constexpr float LOG2E = 1.44269502162933349609375f;
+constexpr double SKEW = 1.3349817e-8;
+constexpr float LOWEST = -3.4028234663852886e38f;   // the reference of nothing: x - LOWEST of x = -inf is -inf, and its exponential 0
+
+__device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
+// 2^u for a row's scalars: reduced in float64, so that what is off is the hardware's exponential on [-1/2, 1/2], 2^-23 of the value
+__device__ __forceinline__ double exp2_d(double u) {
+  u = u < -1200 ? -1200 : u;
+  u = u > 1200 ? 1200 : u;
+  const double n = rint(u);
+  return ldexp((double)exp2_of((float)(u - n)), n == n ? (int)n : 0);
+}
+__device__ __forceinline__ float exp_of(float d) { return exp2_of(d * LOG2E); }
+__device__ __forceinline__ double exp_d(double d) { return exp2_d(d * 1.4426950408889634); }
+// exp(d) - 1 - d, to rounding also where it is small: its series up to 1
+__device__ __forceinline__ double exp_rest(double d) {
+  if (!(fabs(d) <= 1.0)) {
+    const double e = exp_d(d);
+    return e == INFINITY ? INFINITY : e - 1 - d;
+  }
+  const float f = (float)d;
+  float s = 1.f / 479001600;
+  const float c[10] = {1.f / 39916800, 1.f / 3628800, 1.f / 362880, 1.f / 40320, 1.f / 5040, 1.f / 720, 1.f / 120, 1.f / 24, 1.f / 6, 1.f / 2};
+#pragma unroll
+  for (int i = 0; i < 10; i++) s = fmaf(s, f, c[i]);
+  return d * d * (double)s;
+}
+
+template <typename T>
+struct Vec {   // 16 bytes of a row
+  static constexpr int N = 16 / sizeof(T);
+};
+template <typename T>
+__device__ __forceinline__ u32x4 load_vec(const T* p) { return *(const u32x4_any*)p; }
+template <typename T>
+__device__ __forceinline__ void unpack(u32x4 v, float (&f)[Vec<T>::N]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int k = 0; k < 4; k++) f[k] = __uint_as_float(v[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      f[2 * k] = __uint_as_float(v[k] << 16);
+      f[2 * k + 1] = __uint_as_float(v[k] & 0xffff0000u);
+    }
+  }
+}
+// element k becomes minus infinity
+template <typename T>
+__device__ __forceinline__ void take_out(u32x4& v, int k) {
+#pragma unroll
+  for (int d = 0; d < 4; d++) {
+    if constexpr (sizeof(T) == 4) {
+      if (d == k) v[d] = 0xff800000u;
+    } else {
+      if (d == k >> 1) v[d] = k & 1 ? (v[d] & 0xffffu) | 0xff800000u : (v[d] & 0xffff0000u) | 0xff80u;
+    }
+  }
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  bf16x2 o;
+  o[0] = (bf16)a;
+  o[1] = (bf16)b;
+  return __builtin_bit_cast(uint32_t, o);
+}
+// N values of a gradient
+template <typename G, int N>
+__device__ __forceinline__ void store_vec(G* o, const float (&f)[N]) {
+  if constexpr (sizeof(G) == 2 && N == 8) {
+    u32x4 v;
+#pragma unroll
+    for (int k = 0; k < 4; k++) v[k] = pack2(f[2 * k], f[2 * k + 1]);
+    *(u32x4_any*)o = v;
+  } else if constexpr (sizeof(G) == 2) {
+    u32x2 v;
+    v[0] = pack2(f[0], f[1]);
+    v[1] = pack2(f[2], f[3]);
+    *(u32x2_any*)o = v;
+  } else {
+#pragma unroll
+    for (int h = 0; h < N / 4; h++) {
+      u32x4 v;
+#pragma unroll
+      for (int k = 0; k < 4; k++) v[k] = __float_as_uint(f[4 * h + k]);
+      *(u32x4_any*)(o + 4 * h) = v;
+    }
+  }
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// ---- softmax statistics as they run along a row.  m: the reference, at first the maximum of what came first and raised only to what lies far above it (sums of
+// numbers up to 2^16 are as exact as those of numbers up to 1); s = sum exp(x - m); of the first element of each vector, s0 = sum exp(x - m) and t = sum exp(x - m) (x - m).
+struct Run {
+  float m, s, s0, t;
+  __device__ __forceinline__ void start() { m = LOWEST, s = s0 = t = 0.f; }
+  __device__ __forceinline__ float raise(float to) {   // returns the factor
+    const float f = exp_of(m - to);
+    t = f * fmaf(s0, fmaxf(m - to, -1e4f), t);
+    m = to;
+    s *= f;
+    s0 *= f;
+    return f;
+  }
+  __device__ __forceinline__ bool above(float top) const { return top > m + 11.f; }
+  template <int N>
+  __device__ __forceinline__ void add(const float (&f)[N], float (&e)[N]) {   // e: the terms
+#pragma unroll
+    for (int k = 0; k < N; k++) e[k] = exp_of(f[k] - m);
+    t = fmaf(e[0], fmaxf(f[0] - m, -1e4f), t);
+    s0 += e[0];
+    float a = e[0];
+#pragma unroll
+    for (int k = 1; k < N; k++) a += e[k];
+    s += a;
+  }
+  __device__ __forceinline__ void over_wave() {
+    raise(wave_max(m));
+    s = wave_sum(s);
+    s0 = wave_sum(s0);
+    t = wave_sum(t);
+  }
+};
+template <int N>
+__device__ __forceinline__ float max_of(const float (&f)[N]) {
+  float top = f[0];
+#pragma unroll
+  for (int k = 1; k < N; k++) top = fmaxf(top, f[k]);
+  return top;
+}
+// x - y of two logits; minus infinity less itself, of a class that both give probability zero, counts for nothing
+__device__ __forceinline__ float apart(float x, float y) { return __builtin_amdgcn_fmed3f(x - y, -1e30f, 1e30f); }
+// Two rows at once, and kl = sum over x's terms of term * (x - y)
+struct RunPair {
+  Run x, y;
+  float kl;
+  __device__ __forceinline__ void start() { x.start(), y.start(), kl = 0.f; }
+  template <bool FULL, int N>
+  __device__ __forceinline__ void add(const float (&f)[N], const float (&g)[N]) {
+    float e[N];
+    const float top = max_of(f);
+    if (x.above(top)) {
+      const float by = x.raise(top);
+      if (FULL) kl *= by;
+    }
+    x.add(f, e);
+    if (FULL) {
+      const float top_y = max_of(g);
+      if (y.above(top_y)) y.raise(top_y);
+#pragma unroll
+      for (int k = 0; k < N; k++) kl = fmaf(e[k], apart(f[k], g[k]), kl);
+      y.add(g, e);
+    }
+  }
+  template <bool FULL>
+  __device__ __forceinline__ void over_wave() {
+    if (FULL) {
+      const float by = x.raise(wave_max(x.m));
+      kl = wave_sum(kl * by);
+      x.s = wave_sum(x.s);
+      x.s0 = wave_sum(x.s0);
+      x.t = wave_sum(x.t);
+      y.over_wave();
+    } else {
+      x.over_wave();
+    }
+  }
+};
+
+struct RowArgs {
+  const void* logits;
+  long long ld;
+  const int32_t* label;
+  void* grad;
+  long long gld;
+  int rows, classes;
+  __device__ __forceinline__ bool masked(int at) const { return (unsigned)at >= (unsigned)classes; }
+};
+
+struct PolicyArgs {
+  const float *old_logp, *advantage, *ref_logp, *weight;
+  const void* ref;
+  long long ref_ld;
+  double low, high, kl_coef;   // borders of the ratio
+  float* logp;
+};
+
+struct Sequences {
+  const int32_t* offsets;   // or null: every row is one
+  int rows, n;
+  __device__ __forceinline__ int at(int i) const { return offsets ? min(max(offsets[i], 0), rows) : i; }
+};
+struct SeqRows {   // per row, in the workspace
+  double* lp;
+  float *m, *s, *rest;   // (s = 0: masked, or without a distribution)
+  float* g;              // the gradient is g ([j = a] - p[j])
+};
+
+// what a row's statistics come to: s = sum of the terms against m, ea the label's, rest the others', by: what others' terms were multiplied with
+struct RowStat {
+  double s, ea, rest, lp, by;
+  float m;
+  bool none;       // no distribution
+};
+__device__ __forceinline__ RowStat row_stat(const Run& others, float xa) {
+  RowStat o;
+  const double u = (double)xa - (double)others.m, e = exp_d(-fabs(u));
+  const bool above = u > 0;   // (the label becomes the reference)
+  o.m = above ? xa : others.m;
+  o.by = above ? e : 1.0;
+  o.ea = above ? 1.0 : e;
+  o.rest = (double)others.s * o.by;
+  o.s = o.rest + o.ea;
+  o.none = o.s == 0.0;
+  const bool likely = o.ea > o.rest;
+  const double q = o.rest / o.ea, l = log(likely ? 1.0 + q : o.s);
+  o.lp = o.none ? -INFINITY : !likely ? fmin(u, 0.0) - l : -(q < 1e-6 ? q - 0.5 * q * q : l);
+  if (others.s0 > 0.f) o.lp += SKEW * (double)(others.t / others.s0) * (o.rest / o.s);
+  return o;
+}
+
+// what the threads of a row need for its gradient: cf exp(x - m), with the exact divergence (cf + ck ((x - y) - kk)) times that, and `own` for the label.  All zeros: a
+// gradient of zeros.
+struct RowGrad {
+  float m, cf, ck, kk, own;
+};
+
+// Adds a row to the sums (loss, surrogate, divergence, clipped) and says what its gradient is made of
+__device__ __forceinline__ void policy_row(const PolicyArgs& p, const RowStat& s, double* sum, float old, float adv, float ref, double w, RowGrad& o) {
+  if (s.none) return;
+  const double A = (double)adv, ratio = exp_d(s.lp - (double)old);
+  const bool over = (A > 0 && ratio > p.high) || (A < 0 && ratio < p.low);
+  const double surrogate = A * (over ? (A > 0 ? p.high : p.low) : ratio);
+  double g = over ? 0.0 : -ratio * A, kl = 0;
+  if (p.ref_logp) {
+    const double d = (double)ref - s.lp;
+    kl = exp_rest(d);
+    if (p.kl_coef != 0) g -= p.kl_coef * (kl + d);
+  }
+  sum[0] += w * ((p.kl_coef != 0 ? p.kl_coef * kl : 0.0) - surrogate);
+  sum[1] += w * surrogate;
+  sum[2] += w * kl;
+  if (over) sum[3] += w;
+  o.cf = (float)(-w * g / s.s);
+  o.own = (float)(w * g * (s.rest / s.s));
+}
+// the exact divergence on top; log_ratio: log sum exp x - log sum exp y
+__device__ __forceinline__ void full_kl(const PolicyArgs& p, const RowStat& s, double sum_apart, double log_ratio, double* sum, float xa, float ya, double w, RowGrad& o) {
+  if (s.none) return;
+  const double mine = (double)apart(xa, ya), kk = (sum_apart + (s.ea == 0 ? 0.0 : s.ea * mine)) / s.s;
+  const double kl = kk - log_ratio;
+  sum[2] += w * kl;
+  if (p.kl_coef == 0) return;
+  sum[0] += w * p.kl_coef * kl;
+  o.kk = (float)kk;
+  o.ck = (float)(w * p.kl_coef / s.s);
+  if (s.ea != 0) o.own = (float)((double)o.own + w * p.kl_coef * (s.ea / s.s) * (mine - kk));
+}
+
+enum Mode { POLICY, POLICY_FULL, STATS };
+
+constexpr int MAX_GRID = 4096;    // workgroups of the row kernels
+constexpr int COUNT_ROWS = 8192;  // rows that a workgroup counts by itself
+
+// unmasked rows among [begin, end), by all threads of a workgroup; red: one entry for each wave
+__device__ __forceinline__ int count_rows(const RowArgs& a, int begin, int end, int* red) {
+  int n = 0;
+  for (int r = begin + (int)threadIdx.x; r < end; r += blockDim.x) n += a.masked(a.label[r]) ? 0 : 1;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
+  __syncthreads();
+  n = 0;
+  for (int i = 0; i < (int)blockDim.x / 64; i++) n += red[i];
+  return n;
+}
+// ---- rows.  Both kernels below go over the rows r = first, first + step, ...; the threads of a row ("team") are t = 0 .. TPR - 1, and vector v of a row, 16 bytes, is
+// that at element (v * TPR + t) * N of thread t.  A last piece shorter than a vector is one element each of the first threads.
+template <typename T, int W>
+struct RowShape {
+  static constexpr int N = Vec<T>::N, TPR = 64 * W;
+  int C, Cv, rem, nv, mine;   // classes, those in vectors, those behind; vectors of the team, of this thread
+  __device__ __forceinline__ RowShape(int classes, int t) : C(classes), Cv(classes - classes % N), rem(classes % N) {
+    nv = (Cv / N + TPR - 1) / TPR;
+    mine = (Cv / N - t + TPR - 1) / TPR;
+  }
+};
+struct LabelAt {
+  int v, t, k;   // vector, thread and element of a label (v = -1: in the last piece)
+  template <typename T, int W>
+  __device__ __forceinline__ LabelAt(const RowShape<T, W>& s, int at) {
+    constexpr int N = RowShape<T, W>::N, TPR = RowShape<T, W>::TPR;
+    const bool in_vec = at < s.Cv;
+    v = in_vec ? at / N / TPR : -1;
+    t = in_vec ? at / N % TPR : at - s.Cv;
+    k = at % N;
+  }
+};
+
+__device__ __forceinline__ double unit_weight(const RowArgs& a, const int* counts, int n_counts, int* red) {
+  int n = 0;
+  if (n_counts)
+    for (int i = 0; i < n_counts; i++) n += counts[i];
+  else
+    n = count_rows(a, 0, a.rows, red);
+  return 1.0 / n;
+}
+
+// a row's other inputs
+struct RowInputs {
+  float xa, ya, old, adv, ref;
+  double w;
+};
+template <typename T, Mode MODE>
+__device__ __forceinline__ RowInputs row_inputs(const RowArgs& a, const PolicyArgs& p, int r, int at, double unit) {
+  RowInputs o = {0, 0, 0, 0, 0, unit};
+  o.xa = (float)((const T*)a.logits + (long long)r * a.ld)[at];
+  if (MODE == POLICY_FULL) o.ya = (float)((const T*)p.ref + (long long)r * p.ref_ld)[at];
+  if (MODE != STATS) {
+    o.old = p.old_logp[r];
+    o.adv = p.advantage[r];
+    if (p.ref_logp) o.ref = p.ref_logp[r];
+    if (p.weight) o.w = (double)p.weight[r];
+  }
+  return o;
+}
+
+__device__ __forceinline__ void stat_row(const SeqRows& o, int r, const RowStat& s) {
+  o.m[r] = s.m;
+  o.s[r] = (float)s.s;
+  o.rest[r] = (float)s.rest;
+  o.lp[r] = s.none ? 0.0 : s.lp;
+  o.g[r] = 0.f;
+}
+// a masked row, of which nothing is looked at
+template <Mode MODE>
+__device__ __forceinline__ void masked_row(const PolicyArgs& p, const SeqRows& o, int r) {
+  const RowStat none = {0, 0, 0, 0, 0, 0.f, true};
+  if (MODE == STATS) stat_row(o, r, none);
+  else if (p.logp) p.logp[r] = 0.f;
+}
+
+// Adds up a row's statistics over its waves and says what follows from them, in every thread; sums: this team's
+template <int W, Mode MODE>
+__device__ __forceinline__ RowGrad row_scalars(const PolicyArgs& p, const SeqRows& o, int r, RunPair run, const RowInputs& in, RunPair* red, RowGrad* said,
+                                               double* sums) {
+  constexpr bool FULL = MODE == POLICY_FULL;
+  run.over_wave<FULL>();
+  RowGrad b = {0.f, 0.f, 0.f, 0.f, 0.f};
+  if (W > 1) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = run;
+    __syncthreads();
+  }
+  if (W == 1 || threadIdx.x < 64) {
+    const bool first = (threadIdx.x & 63) == 0;
+    if (W > 1) {
+      run.start();
+      if (threadIdx.x < W) run = red[threadIdx.x];
+      run.over_wave<FULL>();
+    }
+    const RowStat s = row_stat(run.x, in.xa);
+    b.m = s.m;
+    if (MODE == STATS) {
+      if (first) stat_row(o, r, s);
+    } else {
+      double sum[4] = {0, 0, 0, 0};
+      policy_row(p, s, sum, in.old, in.adv, in.ref, in.w, b);
+      if (FULL) full_kl(p, s, (double)run.kl * s.by, ((double)s.m - (double)run.y.m) + log(s.s / (double)run.y.s), sum, in.xa, in.ya, in.w, b);
+      if (first) {
+        if (p.logp) p.logp[r] = (float)s.lp;
+#pragma unroll
+        for (int i = 0; i < 4; i++) sums[i] += sum[i];
+      }
+    }
+    if (W > 1 && first) *said = b;
+  }
+  if (W > 1) {
+    __syncthreads();
+    b = *said;
+  }
+  return b;
+}
+
+// ck = 0 without the exact divergence
+template <bool FULL, int N>
+__device__ __forceinline__ void gradient(const RowGrad& b, const float (&f)[N], const float (&g)[N], float (&out)[N]) {
+#pragma unroll
+  for (int k = 0; k < N; k++) {
+    const float e = exp_of(f[k] - b.m);
+    out[k] = e * (FULL ? fmaf(b.ck, apart(f[k], g[k]) - b.kk, b.cf) : b.cf);
+  }
+}
+
+// One row of W waves (W = 1: four rows in a workgroup, a wave each) that stays in registers, at most NV vectors a thread: the logits are read once, and as each
+// vector has become a piece of the gradient the same vector of the next row is loaded in its place, so that loads are on the way all the time, though a row is read and
+// written by turns.  Loads go through buffer descriptors: lanes beyond the row and rows that are not looked at ask for nothing, without a branch around the load (with
+// one the vectors were copied from register to register, which waits for them).
+template <typename T, typename G, int W, int NV, Mode MODE, bool GRAD>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs a, PolicyArgs p, Sequences seq, SeqRows o, const int* __restrict__ counts, int n_counts,
+                                                                        double* __restrict__ parts) {
+  constexpr int N = Vec<T>::N, TPR = 64 * W, TEAMS = W == 1 ? 4 : 1;
+  constexpr bool FULL = MODE == POLICY_FULL;
+  __shared__ RunPair red[W];
+  __shared__ RowGrad said;
+  __shared__ double sums[TEAMS][4];
+  __shared__ int red_n[16];
+  const int t = threadIdx.x % TPR, team = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+  RowShape<T, W> shape(a.classes, t);
+  const int step = gridDim.x * TEAMS;
+  const int begin = MODE == STATS ? seq.at(0) : 0, end = MODE == STATS ? seq.at(seq.n) : a.rows;
+  auto label_of = [&](int r) { return __builtin_amdgcn_readfirstlane(r >= begin && r < end ? a.label[r] : -1); };
+  u32x4 x[NV], y[FULL ? NV : 1];
+  auto source = [&](const void* base, long long ld, int r, bool there) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)((const T*)base + (there ? (long long)r * ld : 0)), 0, there ? shape.Cv * (int)sizeof(T) : 0, 0x00027000);
+  };
+  auto vec_of = [&](__amdgpu_buffer_rsrc_t s, int v) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(s, t * 16, v * TPR * 16, 0)); };
+  int r = blockIdx.x * TEAMS + team, at = r < a.rows ? label_of(r) : -1;
+  {
+    const auto sx = source(a.logits, a.ld, r, !a.masked(at)), sy = source(p.ref, p.ref_ld, r, FULL && !a.masked(at));
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+      x[v] = vec_of(sx, v);
+      if (FULL) y[v] = vec_of(sy, v);
+    }
+  }
+  double unit = 0;   // weight of an unmasked row
+  if (MODE != STATS) {
+    if (threadIdx.x < TEAMS * 4) sums[threadIdx.x / 4][threadIdx.x % 4] = 0;
+    if (!p.weight) unit = unit_weight(a, counts, n_counts, red_n);
+    __syncthreads();
+  }
+  while (r < a.rows) {
+    const int next = (int)min((long long)r + step, (long long)a.rows), next_at = next < a.rows ? label_of(next) : -1;
+    const bool look = !a.masked(at), more = !a.masked(next_at);
+    const auto sx = source(a.logits, a.ld, next, more), sy = source(p.ref, p.ref_ld, next, FULL && more);
+    RowInputs in = {0, 0, 0, 0, 0, 0};
+    float x_tail = -INFINITY, y_tail = -INFINITY;
+    RunPair run;
+    run.start();
+    LabelAt place(shape, at);
+    if (!look) place.v = place.t = -2;
+    asm volatile("" : "+v"(shape.mine));   // (or what is compared with it is kept, in registers that spill)
+    if (look) {
+      in = row_inputs<T, MODE>(a, p, r, at, unit);
+      if (t < shape.rem) {
+        if (!(place.v < 0 && t == place.t)) x_tail = (float)((const T*)a.logits + (long long)r * a.ld)[shape.Cv + t];
+        if (FULL) y_tail = (float)((const T*)p.ref + (long long)r * p.ref_ld)[shape.Cv + t];
+      }
+#pragma unroll
+      for (int v = 0; v < NV; v++)
+        if (v < shape.mine) {
+          if (v == place.v) {
+            if (t == place.t) take_out<T>(x[v], place.k);
+          }
+          float f[N], g[N];
+          unpack<T>(x[v], f);
+          if (FULL) unpack<T>(y[v], g);
+          run.add<FULL>(f, g);
+        }
+      if (t < shape.rem) {
+        const float f[1] = {x_tail}, g[1] = {y_tail};
+        run.add<FULL>(f, g);
+      }
+    }
+    if (!GRAD) {
+#pragma unroll
+      for (int v = 0; v < NV; v++) {
+        x[v] = vec_of(sx, v);
+        if (FULL) y[v] = vec_of(sy, v);
+      }
+    }
+    RowGrad b = {0.f, 0.f, 0.f, 0.f, 0.f};
+    if (look) {
+      b = row_scalars<W, MODE>(p, o, r, run, in, red, &said, sums[team]);
+    } else if (t == 0) {
+      masked_row<MODE>(p, o, r);
+    }
+    if (GRAD) {
+      G* const out = (G*)a.grad + (long long)r * a.gld;
+#pragma unroll
+      for (int v = 0; v < NV; v++) {
+        if (v < shape.mine) {
+          float f[N], g[N], d[N];
+          asm volatile("" : "+v"(x[v]));   // (unpacked again: kept from the first pass it would take twice the registers)
+          unpack<T>(x[v], f);
+          if (FULL) {
+            asm volatile("" : "+v"(y[v]));
+            unpack<T>(y[v], g);
+          }
+          gradient<FULL>(b, f, g, d);
+          if (v == place.v) {
+            if (t == place.t)
+#pragma unroll
+              for (int k = 0; k < N; k++) d[k] = k == place.k ? b.own : d[k];
+          }
+          store_vec<G>(out + v * TPR * N + (unsigned)(t * N), d);
+        }
+        x[v] = vec_of(sx, v);
+        if (FULL) y[v] = vec_of(sy, v);
+      }
+      if (t < shape.rem) {
+        const float f[1] = {look ? x_tail : 0.f}, g[1] = {look ? y_tail : 0.f};
+        float d[1];
+        gradient<FULL>(b, f, g, d);
+        out[shape.Cv + t] = (G)(place.v == -1 && t == place.t ? b.own : d[0]);
+      }
+    }
+    r = next;
+    at = next_at;
+  }
+  if (MODE != STATS) {
+    __syncthreads();
+    if (threadIdx.x < TEAMS * 4) parts[blockIdx.x * TEAMS * 4 + threadIdx.x] = sums[threadIdx.x / 4][threadIdx.x % 4];
+  }
+}
+
+// Rows of any length, U vectors of a thread at a time, read again for the gradient
+template <typename T, typename G, int W, int U, Mode MODE, bool GRAD>
+__global__ __launch_bounds__(64 * W) void streamed_kernel(RowArgs a, PolicyArgs p, Sequences seq, SeqRows o, const int* __restrict__ counts, int n_counts,
+                                                          double* __restrict__ parts) {
+  constexpr int N = Vec<T>::N, TPR = 64 * W;
+  constexpr bool FULL = MODE == POLICY_FULL;
+  __shared__ RunPair red[W];
+  __shared__ RowGrad said;
+  __shared__ double sums[4];
+  __shared__ int red_n[16];
+  const int t = threadIdx.x;
+  const RowShape<T, W> shape(a.classes, t);
+  double unit = 0;
+  if (MODE != STATS) {
+    if (threadIdx.x < 4) sums[threadIdx.x] = 0;
+    if (!p.weight) unit = unit_weight(a, counts, n_counts, red_n);
+    __syncthreads();
+  }
+  const int begin = MODE == STATS ? seq.at(0) : 0, end = MODE == STATS ? seq.at(seq.n) : a.rows;
+  for (int r = blockIdx.x; r < a.rows; r = (int)min((long long)r + gridDim.x, (long long)a.rows)) {
+    const int at = __builtin_amdgcn_readfirstlane(r >= begin && r < end ? a.label[r] : -1);
+    const bool look = !a.masked(at);
+    const T *x = (const T*)a.logits + (long long)r * a.ld, *y = FULL ? (const T*)p.ref + (long long)r * p.ref_ld : x;
+    LabelAt place(shape, at);
+    if (!look) place.v = place.t = -2;
+    RowGrad b = {0.f, 0.f, 0.f, 0.f, 0.f};
+    float x_tail = -INFINITY, y_tail = -INFINITY;
+    if (look) {
+      const RowInputs in = row_inputs<T, MODE>(a, p, r, at, unit);
+      if (t < shape.rem) {
+        if (!(place.v < 0 && t == place.t)) x_tail = (float)x[shape.Cv + t];
+        if (FULL) y_tail = (float)y[shape.Cv + t];
+      }
+      RunPair run;
+      run.start();
+      for (int v = 0; v < shape.nv; v += U) {
+        u32x4 ux[U], uy[FULL ? U : 1];
+#pragma unroll
+        for (int i = 0; i < U; i++)
+          if (v + i < shape.mine) {
+            ux[i] = load_vec(x + (size_t)(v + i) * (TPR * N) + t * N);
+            if (FULL) uy[i] = load_vec(y + (size_t)(v + i) * (TPR * N) + t * N);
+          }
+#pragma unroll
+        for (int i = 0; i < U; i++)
+          if (v + i < shape.mine) {
+            if (v + i == place.v) {
+              if (t == place.t) take_out<T>(ux[i], place.k);
+            }
+            float f[N], g[N];
+            unpack<T>(ux[i], f);
+            if (FULL) unpack<T>(uy[i], g);
+            run.add<FULL>(f, g);
+          }
+      }
+      if (t < shape.rem) {
+        const float f[1] = {x_tail}, g[1] = {y_tail};
+        run.add<FULL>(f, g);
+      }
+      b = row_scalars<W, MODE>(p, o, r, run, in, red, &said, sums);
+    } else if (t == 0) {
+      masked_row<MODE>(p, o, r);
+    }
+    if (!GRAD) continue;
+    G* const out = (G*)a.grad + (long long)r * a.gld;
+    for (int v = 0; v < shape.nv; v += U) {
+      u32x4 ux[U], uy[FULL ? U : 1];
+#pragma unroll
+      for (int i = 0; i < U; i++) {
+        ux[i] = u32x4{0, 0, 0, 0};
+        if (FULL) uy[i] = ux[i];
+        if (look && v + i < shape.mine) {
+          ux[i] = load_vec(x + (size_t)(v + i) * (TPR * N) + t * N);
+          if (FULL) uy[i] = load_vec(y + (size_t)(v + i) * (TPR * N) + t * N);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < U; i++)
+        if (v + i < shape.mine) {
+          float f[N], g[N], d[N];
+          unpack<T>(ux[i], f);
+          if (FULL) unpack<T>(uy[i], g);
+          gradient<FULL>(b, f, g, d);
+          if (v + i == place.v) {
+            if (t == place.t)
+#pragma unroll
+              for (int k = 0; k < N; k++) d[k] = k == place.k ? b.own : d[k];
+          }
+          store_vec<G>(out + (size_t)(v + i) * (TPR * N) + t * N, d);
+        }
+    }
+    if (t < shape.rem) {
+      const float f[1] = {look ? x_tail : 0.f}, g[1] = {look ? y_tail : 0.f};
+      float d[1];
+      gradient<FULL>(b, f, g, d);
+      out[shape.Cv + t] = (G)(place.v == -1 && t == place.t ? b.own : d[0]);
+    }
+  }
+  if (MODE != STATS) {
+    __syncthreads();
+    if (threadIdx.x < 4) parts[blockIdx.x * 4 + threadIdx.x] = sums[threadIdx.x];
+  }
+}
+
+// How rows are taken apart: waves of a row, whether it stays in registers, workgroups on a compute unit
+struct RowPlan {
+  int waves;
+  bool keep;
+  int resident;
+  int teams() const { return waves == 1 ? 4 : 1; }
+};
+// Sixteen vectors a thread (of both rows together) and sixteen waves on a compute unit are what its registers hold.  Where nothing is written rows need not stay, and more
+// of them are on the way at once.
+inline RowPlan row_plan(int classes, size_t size, bool full, bool grad) {
+  const int64_t vecs = ((int64_t)classes * (int64_t)size + 15) / 16, most = full ? 8 : 16;
+  if (vecs <= 64 * (full ? 4 : 8)) return {1, true, 4};
+  if (!grad) return {4, false, full ? 4 : 6};
+  if (vecs <= 256 * most) return {4, true, 4};
+  if (vecs <= 512 * most) return {8, true, 2};
+  if (vecs <= 1024 * most) return {16, true, 1};
+  return {4, false, 4};
+}
+inline int row_grid(int rows, const RowPlan& plan, int cus) { return std::min(std::min(MAX_GRID, cus * plan.resident), (rows - 1) / plan.teams() + 1); }
+
+struct RowCall {
+  RowArgs a;
+  PolicyArgs p;
+  Sequences seq;
+  SeqRows o;
+  const int* counts;
+  int n_counts;
+  double* parts;
+};
+template <typename T, typename G, Mode MODE, bool GRAD>
+void row_launch(const RowPlan& plan, int grid, hipStream_t s, const RowCall& c) {
+  constexpr int F = MODE == POLICY_FULL ? 2 : 1;
+#define ET_ROW(KERNEL, W, NV) \
+  hipLaunchKernelGGL((KERNEL<T, G, W, NV, MODE, GRAD>), dim3(grid), dim3(W == 1 ? 256 : 64 * W), 0, s, c.a, c.p, c.seq, c.o, c.counts, c.n_counts, c.parts)
+  if (!plan.keep) ET_ROW(streamed_kernel, 4, 8 / F);
+  else if (plan.waves == 1) ET_ROW(kept_kernel, 1, 8 / F);
+  else if constexpr (GRAD) {
+    if (plan.waves == 4) ET_ROW(kept_kernel, 4, 16 / F);
+    else if (plan.waves == 8) ET_ROW(kept_kernel, 8, 16 / F);
+    else ET_ROW(kept_kernel, 16, 16 / F);
+  }
+#undef ET_ROW
+}
+
+// the kernels of one type of logits (a translation unit each)
+template <typename T>
+void rows_of_policy(const RowPlan& plan, int grid, hipStream_t s, const RowCall& c, bool grad_bf16);
+template <typename T>
+void rows_of_statistics(const RowPlan& plan, int grid, hipStream_t s, const RowCall& c);
+
+#define ET_ROWS_OF(T)                                                                                                       \
+  template <>                                                                                                               \
+  void rows_of_policy<T>(const RowPlan& plan, int grid, hipStream_t s, const RowCall& c, bool grad_bf16) {                  \
+    if (c.p.ref) {                                                                                                          \
+      if (!c.a.grad) row_launch<T, T, POLICY_FULL, false>(plan, grid, s, c);                                                \
+      else if (grad_bf16) row_launch<T, bf16, POLICY_FULL, true>(plan, grid, s, c);                                         \
+      else row_launch<T, float, POLICY_FULL, true>(plan, grid, s, c);                                                       \
+    } else {                                                                                                                \
+      if (!c.a.grad) row_launch<T, T, POLICY, false>(plan, grid, s, c);                                                     \
+      else if (grad_bf16) row_launch<T, bf16, POLICY, true>(plan, grid, s, c);                                              \
+      else row_launch<T, float, POLICY, true>(plan, grid, s, c);                                                            \
+    }                                                                                                                       \
+  }                                                                                                                         \
+  template <>                                                                                                               \
+  void rows_of_statistics<T>(const RowPlan& plan, int grid, hipStream_t s, const RowCall& c) {                              \
+    row_launch<T, T, STATS, false>(plan, grid, s, c);                                                                       \
+  }
+
+}  // namespace rows
+}  // namespace et
