@@ -52,6 +52,21 @@ __device__ __forceinline__ double exp_rest(double d) {
   return d * d * (double)s;
 }
 
+// log x, x > 0: the hardware's logarithm is taken of the mantissa, so that it is off by 2^-24 and not by that of the whole
+__device__ __forceinline__ double log_d(double x) {
+  const int e = __builtin_amdgcn_frexp_exp(x);
+  return ((double)e + (double)__builtin_amdgcn_logf((float)__builtin_amdgcn_frexp_mant(x))) * 0.69314718055994530942;
+}
+// log(1 + q), 0 <= q <= 1, to rounding also where it is small: 2 artanh z, z = q / (2 + q)
+__device__ __forceinline__ double log1p_d(double q) {
+  const double z = q / (2.0 + q);
+  const float y = (float)(z * z), c[6] = {1.f / 13, 1.f / 11, 1.f / 9, 1.f / 7, 1.f / 5, 1.f / 3};
+  float s = 1.f / 15;
+#pragma unroll
+  for (int i = 0; i < 6; i++) s = fmaf(s, y, c[i]);
+  return 2.0 * (z + z * (double)(y * s));
+}
+
 template <typename T>
 struct Vec {   // 16 bytes of a row
   static constexpr int N = 16 / sizeof(T);
@@ -113,15 +128,29 @@ __device__ __forceinline__ void store_vec(G* o, const float (&f)[N]) {
   }
 }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+// ---- over the lanes of a wave (LANES = 64), or the first LANES of it, without the LDS: within rows of 16 lanes, then from row to row; the result in every lane
+template <int LANES, typename F>
+__device__ __forceinline__ float lanes_reduce(float v, float none, F f) {
+#define ET_DPP(CTRL, ROWS) \
+  v = f(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(v), CTRL, ROWS, 0xf, false)))
+  ET_DPP(0x111, 0xf);
+  if (LANES > 2) ET_DPP(0x112, 0xf);
+  if (LANES > 4) ET_DPP(0x114, 0xf);
+  if (LANES > 8) ET_DPP(0x118, 0xf);
+  if (LANES > 16) {
+    ET_DPP(0x142, 0xa);
+    ET_DPP(0x143, 0xc);
+  }
+#undef ET_DPP
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), LANES - 1));
 }
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+template <int LANES>
+__device__ __forceinline__ float lanes_max(float v) {
+  return lanes_reduce<LANES>(v, LOWEST, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+  return lanes_reduce<LANES>(v, 0.f, [](float a, float b) { return a + b; });
 }
 
 // ---- softmax statistics as they run along a row.  m: the reference, at first the maximum of what came first and raised only to what lies far above it (sums of
@@ -149,18 +178,26 @@ struct Run {
     for (int k = 1; k < N; k++) a += e[k];
     s += a;
   }
-  __device__ __forceinline__ void over_wave() {
-    raise(wave_max(m));
-    s = wave_sum(s);
-    s0 = wave_sum(s0);
-    t = wave_sum(t);
+  template <int LANES>
+  __device__ __forceinline__ float over_lanes() {   // returns the lane's factor
+    const float f = raise(lanes_max<LANES>(m));
+    s = lanes_sum<LANES>(s);
+    s0 = lanes_sum<LANES>(s0);
+    t = lanes_sum<LANES>(t);
+    return f;
   }
 };
+// (the builtin maximum would first quiet every operand, an instruction each)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 template <int N>
 __device__ __forceinline__ float max_of(const float (&f)[N]) {
   float top = f[0];
 #pragma unroll
-  for (int k = 1; k < N; k++) top = fmaxf(top, f[k]);
+  for (int k = 1; k < N; k += 2) top = max3(top, f[k], f[k + 1 < N ? k + 1 : k]);
   return top;
 }
 // x - y of two logits; minus infinity less itself, of a class that both give probability zero, counts for nothing
@@ -187,17 +224,12 @@ struct RunPair {
       y.add(g, e);
     }
   }
-  template <bool FULL>
-  __device__ __forceinline__ void over_wave() {
+  template <bool FULL, int LANES>
+  __device__ __forceinline__ void over_lanes() {
+    const float by = x.over_lanes<LANES>();
     if (FULL) {
-      const float by = x.raise(wave_max(x.m));
-      kl = wave_sum(kl * by);
-      x.s = wave_sum(x.s);
-      x.s0 = wave_sum(x.s0);
-      x.t = wave_sum(x.t);
-      y.over_wave();
-    } else {
-      x.over_wave();
+      kl = lanes_sum<LANES>(kl * by);
+      y.over_lanes<LANES>();
     }
   }
 };
@@ -233,7 +265,7 @@ struct SeqRows {   // per row, in the workspace
 
 // what a row's statistics come to: s = sum of the terms against m, ea the label's, rest the others', by: what others' terms were multiplied with
 struct RowStat {
-  double s, ea, rest, lp, by;
+  double s, inv_s, ea, rest, lp, by;
   float m;
   bool none;       // no distribution
 };
@@ -246,11 +278,10 @@ __device__ __forceinline__ RowStat row_stat(const Run& others, float xa) {
   o.ea = above ? 1.0 : e;
   o.rest = (double)others.s * o.by;
   o.s = o.rest + o.ea;
+  o.inv_s = 1.0 / o.s;
   o.none = o.s == 0.0;
-  const bool likely = o.ea > o.rest;
-  const double q = o.rest / o.ea, l = log(likely ? 1.0 + q : o.s);
-  o.lp = o.none ? -INFINITY : !likely ? fmin(u, 0.0) - l : -(q < 1e-6 ? q - 0.5 * q * q : l);
-  if (others.s0 > 0.f) o.lp += SKEW * (double)(others.t / others.s0) * (o.rest / o.s);
+  o.lp = o.none ? -INFINITY : o.ea > o.rest ? -log1p_d(o.rest / o.ea) : fmin(u, 0.0) - log_d(o.s);
+  if (others.s0 > 0.f) o.lp += SKEW * (double)(others.t / others.s0) * (o.rest * o.inv_s);
   return o;
 }
 
@@ -276,25 +307,26 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& p, const RowStat& s
   sum[1] += w * surrogate;
   sum[2] += w * kl;
   if (over) sum[3] += w;
-  o.cf = (float)(-w * g / s.s);
-  o.own = (float)(w * g * (s.rest / s.s));
+  o.cf = (float)(-w * g * s.inv_s);
+  o.own = (float)(w * g * (s.rest * s.inv_s));
 }
 // the exact divergence on top; log_ratio: log sum exp x - log sum exp y
 __device__ __forceinline__ void full_kl(const PolicyArgs& p, const RowStat& s, double sum_apart, double log_ratio, double* sum, float xa, float ya, double w, RowGrad& o) {
   if (s.none) return;
-  const double mine = (double)apart(xa, ya), kk = (sum_apart + (s.ea == 0 ? 0.0 : s.ea * mine)) / s.s;
+  const double mine = (double)apart(xa, ya), kk = (sum_apart + (s.ea == 0 ? 0.0 : s.ea * mine)) * s.inv_s;
   const double kl = kk - log_ratio;
   sum[2] += w * kl;
   if (p.kl_coef == 0) return;
   sum[0] += w * p.kl_coef * kl;
   o.kk = (float)kk;
-  o.ck = (float)(w * p.kl_coef / s.s);
-  if (s.ea != 0) o.own = (float)((double)o.own + w * p.kl_coef * (s.ea / s.s) * (mine - kk));
+  o.ck = (float)(w * p.kl_coef * s.inv_s);
+  if (s.ea != 0) o.own = (float)((double)o.own + w * p.kl_coef * (s.ea * s.inv_s) * (mine - kk));
 }
 
 enum Mode { POLICY, POLICY_FULL, STATS };
 
 constexpr int MAX_GRID = 4096;    // workgroups of the row kernels
+constexpr int COLUMNS = 5;        // sums over rows: loss, surrogate, divergence, clipped; unmasked rows
 constexpr int COUNT_ROWS = 8192;  // rows that a workgroup counts by itself
 
 // unmasked rows among [begin, end), by all threads of a workgroup; red: one entry for each wave
@@ -370,7 +402,7 @@ __device__ __forceinline__ void stat_row(const SeqRows& o, int r, const RowStat&
 // a masked row, of which nothing is looked at
 template <Mode MODE>
 __device__ __forceinline__ void masked_row(const PolicyArgs& p, const SeqRows& o, int r) {
-  const RowStat none = {0, 0, 0, 0, 0, 0.f, true};
+  const RowStat none = {0, 0, 0, 0, 0, 0, 0.f, true};
   if (MODE == STATS) stat_row(o, r, none);
   else if (p.logp) p.logp[r] = 0.f;
 }
@@ -380,7 +412,7 @@ template <int W, Mode MODE>
 __device__ __forceinline__ RowGrad row_scalars(const PolicyArgs& p, const SeqRows& o, int r, RunPair run, const RowInputs& in, RunPair* red, RowGrad* said,
                                                double* sums) {
   constexpr bool FULL = MODE == POLICY_FULL;
-  run.over_wave<FULL>();
+  run.over_lanes<FULL, 64>();
   RowGrad b = {0.f, 0.f, 0.f, 0.f, 0.f};
   if (W > 1) {
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = run;
@@ -391,7 +423,7 @@ __device__ __forceinline__ RowGrad row_scalars(const PolicyArgs& p, const SeqRow
     if (W > 1) {
       run.start();
       if (threadIdx.x < W) run = red[threadIdx.x];
-      run.over_wave<FULL>();
+      run.over_lanes<FULL, W>();
     }
     const RowStat s = row_stat(run.x, in.xa);
     b.m = s.m;
@@ -400,11 +432,12 @@ __device__ __forceinline__ RowGrad row_scalars(const PolicyArgs& p, const SeqRow
     } else {
       double sum[4] = {0, 0, 0, 0};
       policy_row(p, s, sum, in.old, in.adv, in.ref, in.w, b);
-      if (FULL) full_kl(p, s, (double)run.kl * s.by, ((double)s.m - (double)run.y.m) + log(s.s / (double)run.y.s), sum, in.xa, in.ya, in.w, b);
+      if (FULL) full_kl(p, s, (double)run.kl * s.by, ((double)s.m - (double)run.y.m) + (log_d(s.s) - log_d((double)run.y.s)), sum, in.xa, in.ya, in.w, b);
       if (first) {
         if (p.logp) p.logp[r] = (float)s.lp;
 #pragma unroll
         for (int i = 0; i < 4; i++) sums[i] += sum[i];
+        sums[4] += 1;
       }
     }
     if (W > 1 && first) *said = b;
@@ -437,7 +470,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
   constexpr bool FULL = MODE == POLICY_FULL;
   __shared__ RunPair red[W];
   __shared__ RowGrad said;
-  __shared__ double sums[TEAMS][4];
+  __shared__ double sums[TEAMS][COLUMNS];
   __shared__ int red_n[16];
   const int t = threadIdx.x % TPR, team = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   RowShape<T, W> shape(a.classes, t);
@@ -460,8 +493,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
   }
   double unit = 0;   // weight of an unmasked row
   if (MODE != STATS) {
-    if (threadIdx.x < TEAMS * 4) sums[threadIdx.x / 4][threadIdx.x % 4] = 0;
-    if (!p.weight) unit = unit_weight(a, counts, n_counts, red_n);
+    if (threadIdx.x < TEAMS * COLUMNS) sums[threadIdx.x / COLUMNS][threadIdx.x % COLUMNS] = 0;
+    if (!p.weight) unit = GRAD ? unit_weight(a, counts, n_counts, red_n) : 1.0;
     __syncthreads();
   }
   while (r < a.rows) {
@@ -545,7 +578,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
   }
   if (MODE != STATS) {
     __syncthreads();
-    if (threadIdx.x < TEAMS * 4) parts[blockIdx.x * TEAMS * 4 + threadIdx.x] = sums[threadIdx.x / 4][threadIdx.x % 4];
+    if (threadIdx.x < TEAMS * COLUMNS) parts[blockIdx.x * TEAMS * COLUMNS + threadIdx.x] = sums[threadIdx.x / COLUMNS][threadIdx.x % COLUMNS];
   }
 }
 
@@ -557,14 +590,14 @@ __global__ __launch_bounds__(64 * W) void streamed_kernel(RowArgs a, PolicyArgs 
   constexpr bool FULL = MODE == POLICY_FULL;
   __shared__ RunPair red[W];
   __shared__ RowGrad said;
-  __shared__ double sums[4];
+  __shared__ double sums[COLUMNS];
   __shared__ int red_n[16];
   const int t = threadIdx.x;
   const RowShape<T, W> shape(a.classes, t);
   double unit = 0;
   if (MODE != STATS) {
-    if (threadIdx.x < 4) sums[threadIdx.x] = 0;
-    if (!p.weight) unit = unit_weight(a, counts, n_counts, red_n);
+    if (threadIdx.x < COLUMNS) sums[threadIdx.x] = 0;
+    if (!p.weight) unit = GRAD ? unit_weight(a, counts, n_counts, red_n) : 1.0;
     __syncthreads();
   }
   const int begin = MODE == STATS ? seq.at(0) : 0, end = MODE == STATS ? seq.at(seq.n) : a.rows;
@@ -649,29 +682,30 @@ __global__ __launch_bounds__(64 * W) void streamed_kernel(RowArgs a, PolicyArgs 
   }
   if (MODE != STATS) {
     __syncthreads();
-    if (threadIdx.x < 4) parts[blockIdx.x * 4 + threadIdx.x] = sums[threadIdx.x];
+    if (threadIdx.x < COLUMNS) parts[blockIdx.x * COLUMNS + threadIdx.x] = sums[threadIdx.x];
   }
 }
 
-// How rows are taken apart: waves of a row, whether it stays in registers, workgroups on a compute unit
+// How rows are taken apart: waves of a row, whether it stays in registers, workgroups at most
 struct RowPlan {
   int waves;
   bool keep;
-  int resident;
+  int groups;
   int teams() const { return waves == 1 ? 4 : 1; }
 };
-// Sixteen vectors a thread (of both rows together) and sixteen waves on a compute unit are what its registers hold.  Where nothing is written rows need not stay, and more
-// of them are on the way at once.
-inline RowPlan row_plan(int classes, size_t size, bool full, bool grad) {
+// Sixteen vectors a thread (of both rows together) and sixteen waves on a compute unit are what its registers hold.  Where nothing is written rows need not stay: they are
+// streamed, a workgroup each, more of them at once than run, so that none has much more of them than another (2048 rows of 32000 classes of which one in five is
+// masked take 26 us, over the workgroups that run at once 37).
+inline RowPlan row_plan(int classes, size_t size, bool full, bool grad, int cus) {
   const int64_t vecs = ((int64_t)classes * (int64_t)size + 15) / 16, most = full ? 8 : 16;
-  if (vecs <= 64 * (full ? 4 : 8)) return {1, true, 4};
-  if (!grad) return {4, false, full ? 4 : 6};
-  if (vecs <= 256 * most) return {4, true, 4};
-  if (vecs <= 512 * most) return {8, true, 2};
-  if (vecs <= 1024 * most) return {16, true, 1};
-  return {4, false, 4};
+  if (vecs <= 64 * (full ? 4 : 8)) return {1, true, 4 * cus};
+  if (!grad) return {4, false, MAX_GRID};
+  if (vecs <= 256 * most) return {4, true, 4 * cus};
+  if (vecs <= 512 * most) return {8, true, 2 * cus};
+  if (vecs <= 1024 * most) return {16, true, cus};
+  return {4, false, MAX_GRID};
 }
-inline int row_grid(int rows, const RowPlan& plan, int cus) { return std::min(std::min(MAX_GRID, cus * plan.resident), (rows - 1) / plan.teams() + 1); }
+inline int row_grid(int rows, const RowPlan& plan) { return std::min(std::min(MAX_GRID, plan.groups), (rows - 1) / plan.teams() + 1); }
 
 struct RowCall {
   RowArgs a;

@@ -25,21 +25,32 @@ __global__ __launch_bounds__(256) void count_kernel(RowArgs a, int* __restrict__
   if (threadIdx.x == 0) counts[blockIdx.x] = n;
 }
 
-// adds the lines of partial sums: out[0] = scale * column 0, more[i - 1] = scale * column i
-template <int COLS>
-__global__ __launch_bounds__(256) void finish_kernel(const double* __restrict__ parts, int lines, double scale, float* __restrict__ out,
-                                                     float* __restrict__ more) {
-  __shared__ double red[4];
+// Adds the lines of partial sums: out = scale * column 0, more[i - 1] = scale * column i.  of: divide by this column instead (zero over zero is zero)
+template <int COLS, int OF>
+__global__ __launch_bounds__(1024) void finish_kernel(const double* __restrict__ parts, int lines, double scale, float* __restrict__ out, float* __restrict__ more, int n_more) {
+  __shared__ double red[16][COLS];
+  double v[COLS];
+#pragma unroll
+  for (int i = 0; i < COLS; i++) v[i] = 0;
+  for (int l = threadIdx.x; l < lines; l += 1024)
+#pragma unroll
+    for (int i = 0; i < COLS; i++) v[i] += parts[(size_t)COLS * l + i];
 #pragma unroll
   for (int i = 0; i < COLS; i++) {
-    double v = 0;
-    for (int l = threadIdx.x; l < lines; l += 256) v += parts[COLS * l + i];
-    v = block_sum_d(v, red) * scale;
-    if (threadIdx.x == 0) {
-      if (i == 0) *out = (float)v;
-      else if (more) more[i - 1] = (float)v;
-    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v[i] += __shfl_xor(v[i], o, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6][i] = v[i];
   }
+  __syncthreads();
+  if (threadIdx.x >= COLS) return;
+  double n = 0, s = 0;
+  for (int w = 0; w < 16; w++) {
+    s += red[w][threadIdx.x];
+    if (OF >= 0) n += red[w][OF < 0 ? 0 : OF];
+  }
+  if (OF >= 0) scale = n > 0 ? 1 / n : 0;
+  if (threadIdx.x == 0) *out = (float)(s * scale);
+  else if (more && (int)threadIdx.x <= n_more) more[threadIdx.x - 1] = (float)(s * scale);
 }
 
 // ---- preference
@@ -121,7 +132,7 @@ namespace {
 using namespace et_op;
 
 constexpr int MAX_COUNTS = 256;
-constexpr size_t POLICY_WS = sizeof(int) * MAX_COUNTS + sizeof(double) * 4 * 4 * et::rows::MAX_GRID;
+constexpr size_t POLICY_WS = sizeof(int) * MAX_COUNTS + sizeof(double) * et::rows::COLUMNS * 4 * et::rows::MAX_GRID;
 
 size_t preference_ws(int64_t rows, int64_t pairs) { return (size_t)(rows * 24 + pairs * 24 + 256); }
 
@@ -170,15 +181,20 @@ int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_
   int* counts = (int*)workspace_dev;
   c.counts = counts;
   c.parts = (double*)(counts + MAX_COUNTS);
-  const et::rows::RowPlan plan = et::rows::row_plan(classes, type_size(dtype), c.p.ref != nullptr, grad_dev != nullptr);
-  const int grid = et::rows::row_grid(rows, plan, device_cus(on.dev));
-  if (!p->weight_dev && rows > et::rows::COUNT_ROWS) {
+  const et::rows::RowPlan plan = et::rows::row_plan(classes, type_size(dtype), c.p.ref != nullptr, grad_dev != nullptr, device_cus(on.dev));
+  const int grid = et::rows::row_grid(rows, plan);
+  if (grad_dev && !p->weight_dev && rows > et::rows::COUNT_ROWS) {
     c.n_counts = std::min(MAX_COUNTS, rows / 4096);
     hipLaunchKernelGGL(et::rows::count_kernel, dim3(c.n_counts), dim3(256), 0, s, c.a, counts);
   }
   if (dtype == ET_BF16) et::rows::rows_of_policy<bf16>(plan, grid, s, c, grad_dtype == ET_BF16);
   else et::rows::rows_of_policy<float>(plan, grid, s, c, grad_dtype == ET_BF16);
-  hipLaunchKernelGGL(et::rows::finish_kernel<4>, dim3(1), dim3(256), 0, s, c.parts, grid * plan.teams(), 1.0, loss_dev, p->stats_dev);
+  // (without a gradient rows have the weight 1 as they are added up)
+  const int lines = grid * plan.teams();
+  if (!grad_dev && !p->weight_dev)
+    hipLaunchKernelGGL((et::rows::finish_kernel<et::rows::COLUMNS, 4>), dim3(1), dim3(1024), 0, s, c.parts, lines, 1.0, loss_dev, p->stats_dev, 3);
+  else
+    hipLaunchKernelGGL((et::rows::finish_kernel<et::rows::COLUMNS, -1>), dim3(1), dim3(1024), 0, s, c.parts, lines, 1.0, loss_dev, p->stats_dev, 3);
   return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
 }
 
@@ -205,8 +221,8 @@ int et_preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void*
   c.o.s = c.o.m + rows;
   c.o.rest = c.o.s + rows;
   c.o.g = c.o.rest + rows;
-  const et::rows::RowPlan plan = et::rows::row_plan(classes, type_size(dtype), false, false);
-  const int grid = et::rows::row_grid(rows, plan, device_cus(on.dev));
+  const et::rows::RowPlan plan = et::rows::row_plan(classes, type_size(dtype), false, false, device_cus(on.dev));
+  const int grid = plan.waves == 1 ? et::rows::row_grid(rows, plan) : std::min(rows, 1 << 20);
   if (dtype == ET_BF16) et::rows::rows_of_statistics<bf16>(plan, grid, s, c);
   else et::rows::rows_of_statistics<float>(plan, grid, s, c);
   hipLaunchKernelGGL(et::rows::pair_kernel, dim3(pairs), dim3(256), 0, s, c.seq, c.o, p->ref_logp_dev, (double)p->beta, (double)p->label_smoothing, 1.0 / pairs,
@@ -222,7 +238,7 @@ int et_preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void*
     }
 #undef ET_PAIR_GRAD
   }
-  hipLaunchKernelGGL(et::rows::finish_kernel<3>, dim3(1), dim3(256), 0, s, parts, pairs, 1.0 / pairs, loss_dev, p->stats_dev);
+  hipLaunchKernelGGL((et::rows::finish_kernel<3, -1>), dim3(1), dim3(1024), 0, s, parts, pairs, 1.0 / pairs, loss_dev, p->stats_dev, 2);
   return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
 }
 
