@@ -284,7 +284,7 @@ int et_train_step(et_ctx* ctx, const void* x_dev, const int32_t* y_dev, const ui
  * any state; a call leaves nothing in it that a later one reads.  Calls (and replays of captured ones) that share a workspace must not overlap.
  * Sums run in a fixed order: a call on the same inputs gives the same bits.  ET_ENOMEM: the workspace is too small.
  *
- * Logits: row r of `classes` values starts at logits_dev + r * row_stride (in elements, row_stride >= classes), of type `dtype` (ET_F32 |
+ * Logits: row r of `classes` (at most 2^28) values starts at logits_dev + r * row_stride (in elements, row_stride >= classes), of type `dtype` (ET_F32 |
  * ET_BF16).  The gradient has the same shape, a stride and a type of its own; grad_dev == NULL: no gradient is computed.  It may be logits_dev itself
  * (same stride and type), and must not overlap the logits otherwise (ET_EINVAL).  Pointers need their element's alignment only.  Elements between the rows are
  * neither read nor written.  label_dev[r] is the row's class (the action taken, the token produced); one outside [0, classes) masks the

@@ -17,7 +17,7 @@ namespace rows {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-// Rows start at any element: vectors are loaded and stored at the alignment of an element, which global memory takes on this hardware
+// Vectors are loaded and stored at the alignment of an element, which global memory takes on this hardware
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
 typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -341,26 +341,32 @@ __device__ __forceinline__ int count_rows(const RowArgs& a, int begin, int end, 
   for (int i = 0; i < (int)blockDim.x / 64; i++) n += red[i];
   return n;
 }
-// ---- rows.  Both kernels below go over the rows r = first, first + step, ...; the threads of a row ("team") are t = 0 .. TPR - 1, and vector v of a row, 16 bytes, is
-// that at element (v * TPR + t) * N of thread t.  A last piece shorter than a vector is one element each of the first threads.
+// ---- rows.  Both kernels below go over the rows r = first, first + step, ...; the threads of a row ("team") are t = 0 .. TPR - 1.  Vectors of a row are those that
+// begin at multiples of 16 bytes: vector v of thread t at element head + (v * TPR + t) * N.  What lies in front of the first and behind the last is one element each of the
+// first threads (loads and stores of vectors at any element are right too, and cost 8192 rows of 100003 bf16 classes 10 per cent, and 24 where they are only read).
 template <typename T, int W>
 struct RowShape {
   static constexpr int N = Vec<T>::N, TPR = 64 * W;
-  int C, Cv, rem, nv, mine;   // classes, those in vectors, those behind; vectors of the team, of this thread
-  __device__ __forceinline__ RowShape(int classes, int t) : C(classes), Cv(classes - classes % N), rem(classes % N) {
+  int head, Cv, edge, nv, mine;   // elements in front, in vectors, outside of them; vectors of the team, of this thread
+  __device__ __forceinline__ RowShape(int C, const T* row, int t) {
+    head = min(C, (int)(-(uintptr_t)row & 15) / (int)sizeof(T));
+    Cv = (C - head) / N * N;
+    edge = C - Cv;
     nv = (Cv / N + TPR - 1) / TPR;
     mine = (Cv / N - t + TPR - 1) / TPR;
   }
+  __device__ __forceinline__ int edge_at(int t) const { return t < head ? t : Cv + t; }
 };
 struct LabelAt {
-  int v, t, k;   // vector, thread and element of a label (v = -1: in the last piece)
+  int v, t, k;   // vector, thread and element of a label (v = -1: outside of the vectors)
   template <typename T, int W>
   __device__ __forceinline__ LabelAt(const RowShape<T, W>& s, int at) {
     constexpr int N = RowShape<T, W>::N, TPR = RowShape<T, W>::TPR;
-    const bool in_vec = at < s.Cv;
-    v = in_vec ? at / N / TPR : -1;
-    t = in_vec ? at / N % TPR : at - s.Cv;
-    k = at % N;
+    const int i = at - s.head;
+    const bool in_vec = i >= 0 && i < s.Cv;
+    v = in_vec ? i / N / TPR : -1;
+    t = in_vec ? i / N % TPR : i < 0 ? at : at - s.Cv;
+    k = i & (N - 1);
   }
 };
 
@@ -473,18 +479,23 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
   __shared__ double sums[TEAMS][COLUMNS];
   __shared__ int red_n[16];
   const int t = threadIdx.x % TPR, team = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
-  RowShape<T, W> shape(a.classes, t);
   const int step = gridDim.x * TEAMS;
   const int begin = MODE == STATS ? seq.at(0) : 0, end = MODE == STATS ? seq.at(seq.n) : a.rows;
-  auto label_of = [&](int r) { return __builtin_amdgcn_readfirstlane(r >= begin && r < end ? a.label[r] : -1); };
+  auto label_of = [&](int r) {
+    const int label = a.label[r];
+    return __builtin_amdgcn_readfirstlane(r >= begin && r < end ? label : -1);
+  };
   u32x4 x[NV], y[FULL ? NV : 1];
-  auto source = [&](const void* base, long long ld, int r, bool there) {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)((const T*)base + (there ? (long long)r * ld : 0)), 0, there ? shape.Cv * (int)sizeof(T) : 0, 0x00027000);
+  auto row_x = [&](int r) { return (const T*)a.logits + (long long)r * a.ld; };
+  auto row_y = [&](int r) { return (const T*)p.ref + (long long)r * p.ref_ld; };
+  auto source = [&](const T* row, const RowShape<T, W>& s, bool there) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(row + s.head), 0, there ? s.Cv * (int)sizeof(T) : 0, 0x00027000);
   };
   auto vec_of = [&](__amdgpu_buffer_rsrc_t s, int v) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(s, t * 16, v * TPR * 16, 0)); };
   int r = blockIdx.x * TEAMS + team, at = r < a.rows ? label_of(r) : -1;
+  RowShape<T, W> shape(a.classes, row_x(min(r, a.rows - 1)), t);
   {
-    const auto sx = source(a.logits, a.ld, r, !a.masked(at)), sy = source(p.ref, p.ref_ld, r, FULL && !a.masked(at));
+    const auto sx = source(row_x(min(r, a.rows - 1)), shape, !a.masked(at)), sy = source(row_y(min(r, a.rows - 1)), shape, FULL && !a.masked(at));
 #pragma unroll
     for (int v = 0; v < NV; v++) {
       x[v] = vec_of(sx, v);
@@ -500,9 +511,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
   while (r < a.rows) {
     const int next = (int)min((long long)r + step, (long long)a.rows), next_at = next < a.rows ? label_of(next) : -1;
     const bool look = !a.masked(at), more = !a.masked(next_at);
-    const auto sx = source(a.logits, a.ld, next, more), sy = source(p.ref, p.ref_ld, next, FULL && more);
+    const int then = min(next, a.rows - 1);
+    const RowShape<T, W> shape_then(a.classes, row_x(then), t);
+    const auto sx = source(row_x(then), shape_then, more), sy = source(row_y(then), shape_then, FULL && more);
     RowInputs in = {0, 0, 0, 0, 0, 0};
-    float x_tail = -INFINITY, y_tail = -INFINITY;
+    float x_edge = -INFINITY, y_edge = -INFINITY;
     RunPair run;
     run.start();
     LabelAt place(shape, at);
@@ -510,9 +523,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
     asm volatile("" : "+v"(shape.mine));   // (or what is compared with it is kept, in registers that spill)
     if (look) {
       in = row_inputs<T, MODE>(a, p, r, at, unit);
-      if (t < shape.rem) {
-        if (!(place.v < 0 && t == place.t)) x_tail = (float)((const T*)a.logits + (long long)r * a.ld)[shape.Cv + t];
-        if (FULL) y_tail = (float)((const T*)p.ref + (long long)r * p.ref_ld)[shape.Cv + t];
+      if (t < shape.edge) {
+        if (!(place.v < 0 && t == place.t)) x_edge = (float)row_x(r)[shape.edge_at(t)];
+        if (FULL) y_edge = (float)row_y(r)[shape.edge_at(t)];
       }
 #pragma unroll
       for (int v = 0; v < NV; v++)
@@ -525,8 +538,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
           if (FULL) unpack<T>(y[v], g);
           run.add<FULL>(f, g);
         }
-      if (t < shape.rem) {
-        const float f[1] = {x_tail}, g[1] = {y_tail};
+      if (t < shape.edge) {
+        const float f[1] = {x_edge}, g[1] = {y_edge};
         run.add<FULL>(f, g);
       }
     }
@@ -561,20 +574,21 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
 #pragma unroll
               for (int k = 0; k < N; k++) d[k] = k == place.k ? b.own : d[k];
           }
-          store_vec<G>(out + v * TPR * N + (unsigned)(t * N), d);
+          store_vec<G>(out + shape.head + v * TPR * N + (unsigned)(t * N), d);
         }
         x[v] = vec_of(sx, v);
         if (FULL) y[v] = vec_of(sy, v);
       }
-      if (t < shape.rem) {
-        const float f[1] = {look ? x_tail : 0.f}, g[1] = {look ? y_tail : 0.f};
+      if (t < shape.edge) {
+        const float f[1] = {look ? x_edge : 0.f}, g[1] = {look ? y_edge : 0.f};
         float d[1];
         gradient<FULL>(b, f, g, d);
-        out[shape.Cv + t] = (G)(place.v == -1 && t == place.t ? b.own : d[0]);
+        out[shape.edge_at(t)] = (G)(place.v == -1 && t == place.t ? b.own : d[0]);
       }
     }
     r = next;
     at = next_at;
+    shape = shape_then;
   }
   if (MODE != STATS) {
     __syncthreads();
@@ -582,10 +596,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
   }
 }
 
-// Rows of any length, U vectors of a thread at a time, read again for the gradient
+// Rows of any length, streamed through a window of U vectors a thread: as each has been used the vector U further on is loaded in its place.  Where there is a gradient
+// the row passes twice, and the beginning of the second pass is on the way before the first has ended.
 template <typename T, typename G, int W, int U, Mode MODE, bool GRAD>
-__global__ __launch_bounds__(64 * W) void streamed_kernel(RowArgs a, PolicyArgs p, Sequences seq, SeqRows o, const int* __restrict__ counts, int n_counts,
-                                                          double* __restrict__ parts) {
+__global__ __launch_bounds__(64 * W, 4) void streamed_kernel(RowArgs a, PolicyArgs p, Sequences seq, SeqRows o, const int* __restrict__ counts, int n_counts,
+                                                             double* __restrict__ parts) {
   constexpr int N = Vec<T>::N, TPR = 64 * W;
   constexpr bool FULL = MODE == POLICY_FULL;
   __shared__ RunPair red[W];
@@ -593,7 +608,6 @@ __global__ __launch_bounds__(64 * W) void streamed_kernel(RowArgs a, PolicyArgs 
   __shared__ double sums[COLUMNS];
   __shared__ int red_n[16];
   const int t = threadIdx.x;
-  const RowShape<T, W> shape(a.classes, t);
   double unit = 0;
   if (MODE != STATS) {
     if (threadIdx.x < COLUMNS) sums[threadIdx.x] = 0;
@@ -602,31 +616,38 @@ __global__ __launch_bounds__(64 * W) void streamed_kernel(RowArgs a, PolicyArgs 
   }
   const int begin = MODE == STATS ? seq.at(0) : 0, end = MODE == STATS ? seq.at(seq.n) : a.rows;
   for (int r = blockIdx.x; r < a.rows; r = (int)min((long long)r + gridDim.x, (long long)a.rows)) {
-    const int at = __builtin_amdgcn_readfirstlane(r >= begin && r < end ? a.label[r] : -1);
+    const int label = a.label[r], at = __builtin_amdgcn_readfirstlane(r >= begin && r < end ? label : -1);
     const bool look = !a.masked(at);
     const T *x = (const T*)a.logits + (long long)r * a.ld, *y = FULL ? (const T*)p.ref + (long long)r * p.ref_ld : x;
+    const RowShape<T, W> shape(a.classes, x, t);
+    const int turn = (shape.nv + U - 1) / U * U;   // where the second pass begins
+    const int bytes = look ? shape.Cv * (int)sizeof(T) : 0;
+    const auto sx = __builtin_amdgcn_make_buffer_rsrc((void*)(x + shape.head), 0, bytes, 0x00027000),
+               sy = __builtin_amdgcn_make_buffer_rsrc((void*)(y + shape.head), 0, bytes, 0x00027000);
+    u32x4 ux[U], uy[FULL ? U : 1];
+    auto fetch = [&](int v, int i) {
+      const int at = ((v + i) * TPR + t) * 16;   // (beyond the row: nothing is asked for)
+      ux[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(sx, at, 0, 0));
+      if (FULL) uy[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(sy, at, 0, 0));
+    };
+#pragma unroll
+    for (int i = 0; i < U; i++) fetch(0, i);
     LabelAt place(shape, at);
     if (!look) place.v = place.t = -2;
     RowGrad b = {0.f, 0.f, 0.f, 0.f, 0.f};
-    float x_tail = -INFINITY, y_tail = -INFINITY;
+    float x_edge = -INFINITY, y_edge = -INFINITY;
     if (look) {
       const RowInputs in = row_inputs<T, MODE>(a, p, r, at, unit);
-      if (t < shape.rem) {
-        if (!(place.v < 0 && t == place.t)) x_tail = (float)x[shape.Cv + t];
-        if (FULL) y_tail = (float)y[shape.Cv + t];
+      if (t < shape.edge) {
+        if (!(place.v < 0 && t == place.t)) x_edge = (float)x[shape.edge_at(t)];
+        if (FULL) y_edge = (float)y[shape.edge_at(t)];
       }
       RunPair run;
       run.start();
-      for (int v = 0; v < shape.nv; v += U) {
-        u32x4 ux[U], uy[FULL ? U : 1];
+      for (int v = 0; v < turn; v += U) {
+        const int then = GRAD && v + U == turn ? 0 : v + U;
 #pragma unroll
-        for (int i = 0; i < U; i++)
-          if (v + i < shape.mine) {
-            ux[i] = load_vec(x + (size_t)(v + i) * (TPR * N) + t * N);
-            if (FULL) uy[i] = load_vec(y + (size_t)(v + i) * (TPR * N) + t * N);
-          }
-#pragma unroll
-        for (int i = 0; i < U; i++)
+        for (int i = 0; i < U; i++) {
           if (v + i < shape.mine) {
             if (v + i == place.v) {
               if (t == place.t) take_out<T>(ux[i], place.k);
@@ -636,9 +657,11 @@ __global__ __launch_bounds__(64 * W) void streamed_kernel(RowArgs a, PolicyArgs 
             if (FULL) unpack<T>(uy[i], g);
             run.add<FULL>(f, g);
           }
+          fetch(then, i);
+        }
       }
-      if (t < shape.rem) {
-        const float f[1] = {x_tail}, g[1] = {y_tail};
+      if (t < shape.edge) {
+        const float f[1] = {x_edge}, g[1] = {y_edge};
         run.add<FULL>(f, g);
       }
       b = row_scalars<W, MODE>(p, o, r, run, in, red, &said, sums);
@@ -647,19 +670,9 @@ __global__ __launch_bounds__(64 * W) void streamed_kernel(RowArgs a, PolicyArgs 
     }
     if (!GRAD) continue;
     G* const out = (G*)a.grad + (long long)r * a.gld;
-    for (int v = 0; v < shape.nv; v += U) {
-      u32x4 ux[U], uy[FULL ? U : 1];
+    for (int v = 0; v < turn; v += U)
 #pragma unroll
       for (int i = 0; i < U; i++) {
-        ux[i] = u32x4{0, 0, 0, 0};
-        if (FULL) uy[i] = ux[i];
-        if (look && v + i < shape.mine) {
-          ux[i] = load_vec(x + (size_t)(v + i) * (TPR * N) + t * N);
-          if (FULL) uy[i] = load_vec(y + (size_t)(v + i) * (TPR * N) + t * N);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < U; i++)
         if (v + i < shape.mine) {
           float f[N], g[N], d[N];
           unpack<T>(ux[i], f);
@@ -670,14 +683,15 @@ __global__ __launch_bounds__(64 * W) void streamed_kernel(RowArgs a, PolicyArgs 
 #pragma unroll
               for (int k = 0; k < N; k++) d[k] = k == place.k ? b.own : d[k];
           }
-          store_vec<G>(out + (size_t)(v + i) * (TPR * N) + t * N, d);
+          store_vec<G>(out + shape.head + (size_t)(v + i) * (TPR * N) + t * N, d);
         }
-    }
-    if (t < shape.rem) {
-      const float f[1] = {look ? x_tail : 0.f}, g[1] = {look ? y_tail : 0.f};
+        fetch(v + U, i);
+      }
+    if (t < shape.edge) {
+      const float f[1] = {look ? x_edge : 0.f}, g[1] = {look ? y_edge : 0.f};
       float d[1];
       gradient<FULL>(b, f, g, d);
-      out[shape.Cv + t] = (G)(place.v == -1 && t == place.t ? b.own : d[0]);
+      out[shape.edge_at(t)] = (G)(place.v == -1 && t == place.t ? b.own : d[0]);
     }
   }
   if (MODE != STATS) {

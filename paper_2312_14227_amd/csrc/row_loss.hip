@@ -139,7 +139,7 @@ size_t preference_ws(int64_t rows, int64_t pairs) { return (size_t)(rows * 24 + 
 // the arguments that both losses have in common
 int check_rows(int32_t rows, int32_t classes, const void* logits, int32_t dtype, int64_t stride, const int32_t* label, const void* grad,
                int32_t grad_dtype, int64_t grad_stride, const void* ws, const float* loss) {
-  if (rows < 1 || classes < 1 || !logits || !label || !ws || !loss || !type_ok(dtype) || (grad && !type_ok(grad_dtype))) return ET_EINVAL;
+  if (rows < 1 || classes < 1 || classes > 1 << 28 || !logits || !label || !ws || !loss || !type_ok(dtype) || (grad && !type_ok(grad_dtype))) return ET_EINVAL;
   const int64_t most = (INT64_MAX >> 4) / rows;   // (offsets in bytes stay below 2^62)
   if (stride < classes || stride > most || (grad && (grad_stride < classes || grad_stride > most))) return ET_EINVAL;
   if (!aligned(logits, type_size(dtype)) || !aligned(label, 4) || !aligned(loss, 4) || !aligned(ws, 16)) return ET_EINVAL;

@@ -20,7 +20,7 @@ def _preference(rows=4, pairs=2, classes=10, logits=A, dtype=et.ET_F32, stride=1
     et.et_preference_loss(rows, pairs, classes, logits, dtype, stride, label, et.make_preference(offsets, **kw), grad, gdtype, gstride, ws, need, 0, loss)
 
 
-BOTH = [dict(rows=0), dict(rows=-1), dict(classes=0), dict(logits=0), dict(label=0), dict(ws=0), dict(loss=0), dict(dtype=2), dict(gdtype=7), dict(stride=9),
+BOTH = [dict(rows=0), dict(rows=-1), dict(classes=0), dict(classes=(1 << 28) + 1, stride=1 << 30, gstride=1 << 30), dict(logits=0), dict(label=0), dict(ws=0), dict(loss=0), dict(dtype=2), dict(gdtype=7), dict(stride=9),
         dict(gstride=9), dict(stride=-10), dict(stride=1 << 61), dict(logits=A + 2), dict(grad=2 * A + 2), dict(label=A + 1), dict(loss=A + 2), dict(ws=A + 8),
         dict(dtype=et.ET_BF16, logits=A + 1),
         dict(grad=A, gstride=11),                          # on the logits, with another stride
