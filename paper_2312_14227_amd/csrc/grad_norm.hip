@@ -1,8 +1,9 @@
-// Norm of many gradients as one vector, and clipping by it (et_grad_norm, et_grad_clip).
+// Norm of many gradients as one vector, and clipping by it (et_grad_norm, et_grad_clip, et_grad_scale).
 //
-// Every tensor is cut into chunks, a workgroup per chunk adds its squares in float64, a wave per tensor adds its chunks, one workgroup adds the
-// tensors and derives the coefficient; clipping then goes over the chunks once more.  The table of tensors travels as kernel
-// arguments: nothing is copied from the host.  No atomics: the order of every sum is fixed.
+// Every tensor is cut into chunks, a workgroup adds the squares of each in float64 (a conversion and a fused multiply-add, a quarter of what the vector
+// units do in the time that memory takes), one launch adds the chunks: a workgroup all of them, and one for each tensor its own.  Clipping goes over the chunks once more,
+// from the last to the first, so that what the norm has read last is found in the caches.  The table of tensors travels as kernel arguments: nothing is
+// copied from the host.  No atomics: the order of every sum is fixed.
 #include <cmath>
 
 #include "context.h"
@@ -11,25 +12,57 @@
 namespace et {
 namespace {
 
-constexpr int BATCH = 120;   // tensors per launch (kernel arguments: 32 bytes each)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Tensors of one launch (kernel arguments: at most 4096 bytes)
+constexpr int NORM_BATCH = 196, SCALE_BATCH = 140;
+template <int BATCH>
 struct Tensors {
-  int n, first;              // tensors of this launch, and the index of the first
-  uint32_t chunk;            // elements of a chunk
-  uint32_t begin[BATCH + 1]; // first chunk of each, counted over all launches
+  int n, first;               // how many, and the index of the first
+  uint32_t chunk;             // elements of a chunk, a multiple of 16
+  uint32_t begin[BATCH + 1];  // first chunk of each, counted over all launches
   const void* g[BATCH];
-  void* out[BATCH];
   uint64_t numel[BATCH];
 };
+struct ScaleTensors : Tensors<SCALE_BATCH> {
+  void* out[SCALE_BATCH];
+};
 
-// the tensor that a chunk belongs to: the last that begins at or in front of it and is not empty
-__device__ __forceinline__ int tensor_of(const Tensors& t, uint32_t chunk) {
-  int lo = 0, hi = t.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (t.begin[mid] <= chunk) lo = mid;
-    else hi = mid - 1;
+// the tensor that a chunk belongs to: as many as begin at or in front of it, less one (every wave asks for the whole table at once)
+template <int BATCH>
+__device__ __forceinline__ int tensor_of(const Tensors<BATCH>& t, uint32_t chunk) {
+  int k = -1;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < BATCH; i += 64) k += __popcll(__ballot(i + lane < t.n && i + lane < BATCH && t.begin[i + lane < BATCH ? i + lane : 0] <= chunk));
+  return __builtin_amdgcn_readfirstlane(k);
+}
+
+// A chunk as vectors that begin at multiples of 16 bytes, and single elements in front of and behind them
+template <typename T>
+struct Piece {
+  static constexpr int N = 16 / sizeof(T);
+  const T* g;
+  int n, head, vecs, edge;
+  __device__ __forceinline__ Piece(const T* at, int count) : g(at), n(count) {
+    head = min(n, (int)(-(uintptr_t)at & 15) / (int)sizeof(T));
+    vecs = (n - head) / N;
+    edge = n - vecs * N;
   }
-  return lo;
+  __device__ __forceinline__ int edge_at(int i) const { return i < head ? i : vecs * N + i; }
+  __device__ __forceinline__ const u32x4* vec() const { return (const u32x4*)(g + head); }
+};
+template <typename T, int BATCH>
+__device__ __forceinline__ Piece<T> piece_of(const Tensors<BATCH>& t, int k, uint32_t chunk) {
+  const uint64_t off = (uint64_t)(chunk - t.begin[k]) * t.chunk;
+  return Piece<T>((const T*)t.g[k] + off, (int)min((uint64_t)t.chunk, t.numel[k] - off));
+}
+template <typename T>
+__device__ __forceinline__ float value(u32x4 v, int k) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(v[k]);
+  else return __uint_as_float(k & 1 ? v[k >> 1] & 0xffff0000u : v[k >> 1] << 16);
 }
 
 __device__ __forceinline__ double wave_sum_d(double v) {
@@ -37,47 +70,59 @@ __device__ __forceinline__ double wave_sum_d(double v) {
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
 }
+template <int WAVES>
 __device__ __forceinline__ double block_sum_d(double v, double* red) {
   v = wave_sum_d(v);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
+  v = red[0];
+  for (int w = 1; w < WAVES; w++) v += red[w];
+  return v;
 }
 
+constexpr int VECS = 8;   // of a thread, on the way at once
+
 template <typename T>
-__global__ __launch_bounds__(256) void squares_kernel(Tensors t, double* __restrict__ part) {
+__global__ __launch_bounds__(256) void squares_kernel(Tensors<NORM_BATCH> t, double* __restrict__ part, uint32_t* __restrict__ begin) {
   __shared__ double red[4];
   const uint32_t c = t.begin[0] + blockIdx.x;
   const int k = tensor_of(t, c);
-  const uint64_t off = (uint64_t)(c - t.begin[k]) * t.chunk;
-  const T* g = (const T*)t.g[k] + off;
-  const uint32_t n = (uint32_t)min((uint64_t)t.chunk, t.numel[k] - off);
-  double s = 0;
-  for (uint32_t i = threadIdx.x; i < n; i += 256) {
-    const double v = (double)(float)g[i];
-    s += v * v;
+  const Piece<T> p = piece_of<T>(t, k, c);
+  double s0 = 0, s1 = 0;
+  for (int v0 = threadIdx.x; v0 < p.vecs; v0 += 256 * VECS) {
+    u32x4 v[VECS];
+#pragma unroll
+    for (int i = 0; i < VECS; i++) v[i] = v0 + 256 * i < p.vecs ? __builtin_nontemporal_load(p.vec() + v0 + 256 * i) : u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < VECS; i++)
+#pragma unroll
+      for (int e = 0; e < Piece<T>::N; e += 2) {
+        const double a = (double)value<T>(v[i], e), b = (double)value<T>(v[i], e + 1);
+        s0 = fma(a, a, s0);
+        s1 = fma(b, b, s1);
+      }
   }
-  s = block_sum_d(s, red);
-  if (threadIdx.x == 0) part[c] = s;
+  if ((int)threadIdx.x < p.edge) {
+    const double a = (double)(float)p.g[p.edge_at(threadIdx.x)];
+    s0 = fma(a, a, s0);
+  }
+  const double s = block_sum_d<4>(s0 + s1, red);
+  if (threadIdx.x == 0 && p.n > 0) part[c] = s;   // (a launch of empty tensors has a workgroup, but no chunk)
+  // what the next launch needs of the table
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < t.n; i += gridDim.x * 256) begin[t.first + i] = t.begin[i];
 }
 
-__global__ __launch_bounds__(64) void tensor_kernel(Tensors t, const double* __restrict__ part, double* __restrict__ squares, float* __restrict__ norm) {
-  const int k = blockIdx.x;
+// workgroup 0: the norm of all; k + 1: of tensor k
+__global__ __launch_bounds__(1024) void norms_kernel(const double* __restrict__ part, const uint32_t* __restrict__ begin, int n, uint32_t chunks, float* __restrict__ norm,
+                                                     float* __restrict__ tensor_norm) {
+  __shared__ double red[16];
+  const int k = (int)blockIdx.x - 1;
+  const uint32_t from = k < 0 ? 0 : begin[k], to = k < 0 || k + 1 == n ? chunks : begin[k + 1];
   double s = 0;
-  for (uint32_t c = t.begin[k] + threadIdx.x; c < t.begin[k + 1]; c += 64) s += part[c];
-  s = wave_sum_d(s);
-  if (threadIdx.x == 0) {
-    squares[t.first + k] = s;
-    if (norm) norm[t.first + k] = (float)sqrt(s);
-  }
-}
-
-__global__ __launch_bounds__(256) void norm_kernel(const double* __restrict__ squares, int n, float* __restrict__ norm) {
-  __shared__ double red[4];
-  double s = 0;
-  for (int i = threadIdx.x; i < n; i += 256) s += squares[i];
-  s = block_sum_d(s, red);
-  if (threadIdx.x == 0) *norm = (float)sqrt(s);
+#pragma unroll 4
+  for (uint32_t c = from + threadIdx.x; c < to; c += 1024) s += part[c];
+  s = block_sum_d<16>(s, red);
+  if (threadIdx.x == 0) (k < 0 ? norm[0] : tensor_norm[k]) = (float)sqrt(s);
 }
 
 __device__ __forceinline__ float clip_scale(float norm, float max_norm) {
@@ -85,16 +130,40 @@ __device__ __forceinline__ float clip_scale(float norm, float max_norm) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void scale_kernel(Tensors t, const float* __restrict__ norm, float max_norm) {
-  const uint32_t c = t.begin[0] + blockIdx.x;
+__global__ __launch_bounds__(256) void scale_kernel(ScaleTensors t, const float* __restrict__ norm, float max_norm) {
+  const uint32_t c = t.begin[t.n] - 1 - blockIdx.x;
   const int k = tensor_of(t, c);
   const float f = clip_scale(*norm, max_norm);
   if (f == 1.f && t.out[k] == t.g[k]) return;
-  const uint64_t off = (uint64_t)(c - t.begin[k]) * t.chunk;
-  const T* g = (const T*)t.g[k] + off;
-  T* o = (T*)t.out[k] + off;
-  const uint32_t n = (uint32_t)min((uint64_t)t.chunk, t.numel[k] - off);
-  for (uint32_t i = threadIdx.x; i < n; i += 256) o[i] = f == 1.f ? g[i] : (T)((float)g[i] * f);
+  const Piece<T> p = piece_of<T>(t, k, c);
+  T* const o = (T*)t.out[k] + (p.g - (const T*)t.g[k]);
+  for (int v0 = threadIdx.x; v0 < p.vecs; v0 += 256 * VECS) {
+    u32x4 v[VECS];
+#pragma unroll
+    for (int i = 0; i < VECS; i++)
+      if (v0 + 256 * i < p.vecs) v[i] = p.vec()[v0 + 256 * i];
+#pragma unroll
+    for (int i = 0; i < VECS; i++) {
+      if (v0 + 256 * i >= p.vecs) break;
+      u32x4 w;
+#pragma unroll
+      for (int d = 0; d < 4; d++) {
+        if constexpr (sizeof(T) == 4) {
+          w[d] = __float_as_uint(value<T>(v[i], d) * f);
+        } else {
+          bf16x2 b;
+          b[0] = (bf16)(value<T>(v[i], 2 * d) * f);
+          b[1] = (bf16)(value<T>(v[i], 2 * d + 1) * f);
+          w[d] = __builtin_bit_cast(uint32_t, b);
+        }
+      }
+      __builtin_nontemporal_store(w, (u32x4_any*)(o + p.head) + v0 + 256 * i);
+    }
+  }
+  if ((int)threadIdx.x < p.edge) {
+    const int j = p.edge_at(threadIdx.x);
+    o[j] = (T)((float)p.g[j] * f);
+  }
 }
 
 }  // namespace
@@ -106,19 +175,21 @@ using namespace et_op;
 
 struct Plan {
   uint64_t total = 0, chunks = 0;
-  uint32_t chunk = 16384;
+  uint32_t chunk = 4096;
 };
 
-// false: a size that no memory holds
+// False: a size that no memory holds.  Chunks of 64 KB where there are enough of them, so that a workgroup's beginning and end are a small part of it;
+// smaller ones spread few elements over the chip (200 000 of them: 49 workgroups of 4096, 6.0 us, or 13 of 16384, 7.5); larger ones keep the sums of chunks few.
 bool make_plan(int32_t n, const uint64_t* numel, Plan* p) {
   for (int32_t i = 0; i < n; i++) {
     if (numel[i] > (1ull << 48) || (p->total += numel[i]) > (1ull << 48)) return false;
   }
+  while (p->chunk < 16384 && p->total / p->chunk > 1024) p->chunk *= 2;
   while (p->chunk < (1u << 30) && p->total / p->chunk > 65536) p->chunk *= 2;
   for (int32_t i = 0; i < n; i++) p->chunks += (numel[i] + p->chunk - 1) / p->chunk;
   return p->chunks < (1ull << 31);
 }
-size_t ws_bytes(int32_t n, const Plan& p) { return 64 + sizeof(double) * ((size_t)n + p.chunks); }
+size_t ws_bytes(int32_t n, const Plan& p) { return 64 + sizeof(double) * (size_t)p.chunks + sizeof(uint32_t) * (size_t)n; }
 
 int check_tensors(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, int32_t dtype, const float* norm) {
   if (n < 0 || (n > 0 && (!grad || !numel)) || !type_ok(dtype) || !norm || !aligned(norm, 4)) return ET_EINVAL;
@@ -132,48 +203,48 @@ int check_tensors(int32_t n, const void* const* grad, void* const* out, const ui
   return ET_OK;
 }
 
-// calls f(table, workgroups) for every launch over the chunks
-template <typename F>
-void each_batch(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, const Plan& p, F f) {
-  uint32_t next = 0;
-  for (int32_t i0 = 0; i0 < n; i0 += et::BATCH) {
-    et::Tensors t;
-    t.n = std::min<int32_t>(et::BATCH, n - i0);
-    t.first = i0;
-    t.chunk = p.chunk;
-    for (int k = 0; k < t.n; k++) {
-      t.begin[k] = next;
-      t.g[k] = grad[i0 + k];
-      t.out[k] = out ? out[i0 + k] : const_cast<void*>(grad[i0 + k]);
-      t.numel[k] = numel[i0 + k];
-      next += (uint32_t)((numel[i0 + k] + p.chunk - 1) / p.chunk);
-    }
-    t.begin[t.n] = next;
-    f(t, next - t.begin[0]);
+// fills the table of the launch that begins with tensor `first`; next: its first chunk, and what follows its last
+template <int BATCH>
+void fill(et::Tensors<BATCH>* t, int32_t n, int32_t first, const void* const* grad, const uint64_t* numel, const Plan& p, uint32_t* next) {
+  t->n = std::min<int32_t>(BATCH, n - first);
+  t->first = first;
+  t->chunk = p.chunk;
+  for (int k = 0; k < t->n; k++) {
+    t->begin[k] = *next;
+    t->g[k] = grad[first + k];
+    t->numel[k] = numel[first + k];
+    *next += (uint32_t)((numel[first + k] + p.chunk - 1) / p.chunk);
   }
+  t->begin[t->n] = *next;
 }
 
 void norm_launch(int32_t n, const void* const* grad, const uint64_t* numel, int32_t dtype, const Plan& p, void* ws, hipStream_t s, float* norm,
                  float* tensor_norm) {
-  double* squares = (double*)ws;
-  double* part = squares + n;
-  each_batch(n, grad, nullptr, numel, p, [&](const et::Tensors& t, uint32_t grid) {
-    if (grid) {
-      if (dtype == ET_BF16) hipLaunchKernelGGL(et::squares_kernel<bf16>, dim3(grid), dim3(256), 0, s, t, part);
-      else hipLaunchKernelGGL(et::squares_kernel<float>, dim3(grid), dim3(256), 0, s, t, part);
-    }
-    hipLaunchKernelGGL(et::tensor_kernel, dim3(t.n), dim3(64), 0, s, t, part, squares, tensor_norm);
-  });
-  hipLaunchKernelGGL(et::norm_kernel, dim3(1), dim3(256), 0, s, squares, n, norm);
+  double* part = (double*)ws;
+  uint32_t* begin = (uint32_t*)(part + p.chunks);
+  uint32_t next = 0;
+  for (int32_t first = 0; first < n; first += et::NORM_BATCH) {
+    et::Tensors<et::NORM_BATCH> t;
+    fill(&t, n, first, grad, numel, p, &next);
+    const uint32_t grid = std::max(1u, next - t.begin[0]);
+    if (dtype == ET_BF16) hipLaunchKernelGGL(et::squares_kernel<bf16>, dim3(grid), dim3(256), 0, s, t, part, begin);
+    else hipLaunchKernelGGL(et::squares_kernel<float>, dim3(grid), dim3(256), 0, s, t, part, begin);
+  }
+  hipLaunchKernelGGL(et::norms_kernel, dim3(tensor_norm ? n + 1 : 1), dim3(1024), 0, s, part, begin, n, (uint32_t)p.chunks, norm, tensor_norm);
 }
 
 void scale_launch(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, int32_t dtype, const Plan& p, const float* norm, float max_norm,
                   hipStream_t s) {
-  each_batch(n, grad, out, numel, p, [&](const et::Tensors& t, uint32_t grid) {
-    if (!grid) return;
-    if (dtype == ET_BF16) hipLaunchKernelGGL(et::scale_kernel<bf16>, dim3(grid), dim3(256), 0, s, t, norm, max_norm);
-    else hipLaunchKernelGGL(et::scale_kernel<float>, dim3(grid), dim3(256), 0, s, t, norm, max_norm);
-  });
+  for (int32_t i = (n - 1) / et::SCALE_BATCH; n > 0 && i >= 0; i--) {
+    et::ScaleTensors t;
+    uint32_t next = 0;
+    const int32_t first = i * et::SCALE_BATCH;
+    fill(&t, n, first, grad, numel, p, &next);
+    for (int k = 0; k < t.n; k++) t.out[k] = out ? out[first + k] : const_cast<void*>(grad[first + k]);
+    if (!next) continue;
+    if (dtype == ET_BF16) hipLaunchKernelGGL(et::scale_kernel<bf16>, dim3(next), dim3(256), 0, s, t, norm, max_norm);
+    else hipLaunchKernelGGL(et::scale_kernel<float>, dim3(next), dim3(256), 0, s, t, norm, max_norm);
+  }
 }
 
 // max_norm < 0: the norm only
