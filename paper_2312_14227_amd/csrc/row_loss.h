@@ -8,6 +8,7 @@
 // gradient 8 more; a row of 128000 bf16 classes takes a compute unit 18 us of those and 24 us of its share of the memory.
 #pragma once
 #include <cmath>
+#include <type_traits>
 
 #include "context.h"
 #include "op_args.h"
@@ -104,26 +105,31 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   o[1] = (bf16)b;
   return __builtin_bit_cast(uint32_t, o);
 }
+template <bool NT, typename V, typename P>
+__device__ __forceinline__ void put(V v, P* at) {
+  if (NT) __builtin_nontemporal_store(v, at);
+  else *at = v;
+}
 // N values of a gradient
-template <typename G, int N>
+template <typename G, bool NT = false, int N>
 __device__ __forceinline__ void store_vec(G* o, const float (&f)[N]) {
   if constexpr (sizeof(G) == 2 && N == 8) {
     u32x4 v;
 #pragma unroll
     for (int k = 0; k < 4; k++) v[k] = pack2(f[2 * k], f[2 * k + 1]);
-    *(u32x4_any*)o = v;
+    put<NT>(v, (u32x4_any*)o);
   } else if constexpr (sizeof(G) == 2) {
     u32x2 v;
     v[0] = pack2(f[0], f[1]);
     v[1] = pack2(f[2], f[3]);
-    *(u32x2_any*)o = v;
+    put<NT>(v, (u32x2_any*)o);
   } else {
 #pragma unroll
     for (int h = 0; h < N / 4; h++) {
       u32x4 v;
 #pragma unroll
       for (int k = 0; k < 4; k++) v[k] = __float_as_uint(f[4 * h + k]);
-      *(u32x4_any*)(o + 4 * h) = v;
+      put<NT>(v, (u32x4_any*)(o + 4 * h));
     }
   }
 }
@@ -323,6 +329,8 @@ __device__ __forceinline__ void full_kl(const PolicyArgs& p, const RowStat& s, d
   if (s.ea != 0) o.own = (float)((double)o.own + w * p.kl_coef * (s.ea * s.inv_s) * (mine - kk));
 }
 
+constexpr int AUX_NT = 2;   // cache policy of a buffer load: non-temporal
+
 enum Mode { POLICY, POLICY_FULL, STATS };
 
 constexpr int MAX_GRID = 4096;    // workgroups of the row kernels
@@ -469,7 +477,8 @@ __device__ __forceinline__ void gradient(const RowGrad& b, const float (&f)[N], 
 // vector has become a piece of the gradient the same vector of the next row is loaded in its place, so that loads are on the way all the time, though a row is read and
 // written by turns.  Loads go through buffer descriptors: lanes beyond the row and rows that are not looked at ask for nothing, without a branch around the load (with
 // one the vectors were copied from register to register, which waits for them).
-template <typename T, typename G, int W, int NV, Mode MODE, bool GRAD>
+// NT: past the caches, both ways.
+template <typename T, typename G, int W, int NV, Mode MODE, bool GRAD, bool NT>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs a, PolicyArgs p, Sequences seq, SeqRows o, const int* __restrict__ counts, int n_counts,
                                                                         double* __restrict__ parts) {
   constexpr int N = Vec<T>::N, TPR = 64 * W, TEAMS = W == 1 ? 4 : 1;
@@ -491,7 +500,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
   auto source = [&](const T* row, const RowShape<T, W>& s, bool there) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)(row + s.head), 0, there ? s.Cv * (int)sizeof(T) : 0, 0x00027000);
   };
-  auto vec_of = [&](__amdgpu_buffer_rsrc_t s, int v) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(s, t * 16, v * TPR * 16, 0)); };
+  auto vec_of = [&](__amdgpu_buffer_rsrc_t s, int v) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(s, t * 16, v * TPR * 16, NT ? AUX_NT : 0)); };
   int r = blockIdx.x * TEAMS + team, at = r < a.rows ? label_of(r) : -1;
   RowShape<T, W> shape(a.classes, row_x(min(r, a.rows - 1)), t);
   {
@@ -574,7 +583,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
 #pragma unroll
               for (int k = 0; k < N; k++) d[k] = k == place.k ? b.own : d[k];
           }
-          store_vec<G>(out + shape.head + v * TPR * N + (unsigned)(t * N), d);
+          store_vec<G, NT>(out + shape.head + v * TPR * N + (unsigned)(t * N), d);
         }
         x[v] = vec_of(sx, v);
         if (FULL) y[v] = vec_of(sy, v);
@@ -598,7 +607,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
 
 // Rows of any length, streamed through a window of U vectors a thread: as each has been used the vector U further on is loaded in its place.  Where there is a gradient
 // the row passes twice, and the beginning of the second pass is on the way before the first has ended.
-template <typename T, typename G, int W, int U, Mode MODE, bool GRAD>
+template <typename T, typename G, int W, int U, Mode MODE, bool GRAD, bool NT>
 __global__ __launch_bounds__(64 * W, 4) void streamed_kernel(RowArgs a, PolicyArgs p, Sequences seq, SeqRows o, const int* __restrict__ counts, int n_counts,
                                                              double* __restrict__ parts) {
   constexpr int N = Vec<T>::N, TPR = 64 * W;
@@ -627,8 +636,8 @@ __global__ __launch_bounds__(64 * W, 4) void streamed_kernel(RowArgs a, PolicyAr
     u32x4 ux[U], uy[FULL ? U : 1];
     auto fetch = [&](int v, int i) {
       const int at = ((v + i) * TPR + t) * 16;   // (beyond the row: nothing is asked for)
-      ux[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(sx, at, 0, 0));
-      if (FULL) uy[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(sy, at, 0, 0));
+      ux[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(sx, at, 0, NT ? AUX_NT : 0));
+      if (FULL) uy[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(sy, at, 0, NT ? AUX_NT : 0));
     };
 #pragma unroll
     for (int i = 0; i < U; i++) fetch(0, i);
@@ -700,24 +709,31 @@ __global__ __launch_bounds__(64 * W, 4) void streamed_kernel(RowArgs a, PolicyAr
   }
 }
 
-// How rows are taken apart: waves of a row, whether it stays in registers, workgroups at most
+// How rows are taken apart: waves of a row, whether it stays in registers, workgroups at most, whether past the caches
 struct RowPlan {
   int waves;
   bool keep;
   int groups;
+  bool nt;
   int teams() const { return waves == 1 ? 4 : 1; }
 };
 // Sixteen vectors a thread (of both rows together) and sixteen waves on a compute unit are what its registers hold.  Where nothing is written rows need not stay: they are
 // streamed, a workgroup each, more of them at once than run, so that none has much more of them than another (2048 rows of 32000 classes of which one in five is
 // masked take 26 us, over the workgroups that run at once 37).
-inline RowPlan row_plan(int classes, size_t size, bool full, bool grad, int cus) {
+// Past the caches goes what is read once: statistics of 7148 rows of 100003 classes 198 us instead of 228, the whole preference loss 632 instead of 662.  What the last-level
+// cache holds (256 MB) until the gradient's pass or the next kernel reads it is left there: four short pairs of 32000 classes, 63 MB, would take 45 us instead of 40.  Loads and stores
+// of gradients that it cannot hold: exact divergence of 4096 rows of 50257 classes 265 us instead of 273, policy loss of 8192 of 128000 815 instead of 823.
+constexpr double CACHED = 192e6;
+inline RowPlan row_plan(int rows, int classes, size_t size, bool full, bool grad, bool again, int cus) {
   const int64_t vecs = ((int64_t)classes * (int64_t)size + 15) / 16, most = full ? 8 : 16;
-  if (vecs <= 64 * (full ? 4 : 8)) return {1, true, 4 * cus};
-  if (!grad) return {4, false, MAX_GRID};
-  if (vecs <= 256 * most) return {4, true, 4 * cus};
-  if (vecs <= 512 * most) return {8, true, 2 * cus};
-  if (vecs <= 1024 * most) return {16, true, cus};
-  return {4, false, MAX_GRID};
+  const double bytes = (double)rows * classes * size;
+  if (vecs <= 64 * (full ? 4 : 8)) return {1, true, 4 * cus, false};
+  if (!grad) return {4, false, MAX_GRID, !again || bytes > CACHED};
+  const bool nt = bytes > CACHED;
+  if (vecs <= 256 * most) return {4, true, 4 * cus, nt};
+  if (vecs <= 512 * most) return {8, true, 2 * cus, nt};
+  if (vecs <= 1024 * most) return {16, true, cus, nt};
+  return {4, false, MAX_GRID, false};
 }
 inline int row_grid(int rows, const RowPlan& plan) { return std::min(std::min(MAX_GRID, plan.groups), (rows - 1) / plan.teams() + 1); }
 
@@ -733,14 +749,25 @@ struct RowCall {
 template <typename T, typename G, Mode MODE, bool GRAD>
 void row_launch(const RowPlan& plan, int grid, hipStream_t s, const RowCall& c) {
   constexpr int F = MODE == POLICY_FULL ? 2 : 1;
-#define ET_ROW(KERNEL, W, NV) \
-  hipLaunchKernelGGL((KERNEL<T, G, W, NV, MODE, GRAD>), dim3(grid), dim3(W == 1 ? 256 : 64 * W), 0, s, c.a, c.p, c.seq, c.o, c.counts, c.n_counts, c.parts)
-  if (!plan.keep) ET_ROW(streamed_kernel, 4, 8 / F);
-  else if (plan.waves == 1) ET_ROW(kept_kernel, 1, 8 / F);
-  else if constexpr (GRAD) {
-    if (plan.waves == 4) ET_ROW(kept_kernel, 4, 16 / F);
-    else if (plan.waves == 8) ET_ROW(kept_kernel, 8, 16 / F);
-    else ET_ROW(kept_kernel, 16, 16 / F);
+#define ET_ROW(KERNEL, W, NV, NT) \
+  hipLaunchKernelGGL((KERNEL<T, G, W, NV, MODE, GRAD, NT>), dim3(grid), dim3(W == 1 ? 256 : 64 * W), 0, s, c.a, c.p, c.seq, c.o, c.counts, c.n_counts, c.parts)
+  constexpr bool SAME = std::is_same<T, G>::value;   // (a gradient of another type than the logits is rare: not both kinds of kernels)
+  if (plan.waves == 1) {
+    if (c.a.classes * sizeof(T) <= 64 * 16 * 2) ET_ROW(kept_kernel, 1, 2, false);
+    else ET_ROW(kept_kernel, 1, 8 / F, false);
+  } else if constexpr (!GRAD) {
+    if (plan.nt) ET_ROW(streamed_kernel, 4, 8 / F, true);
+    else ET_ROW(streamed_kernel, 4, 8 / F, false);
+  } else if (!plan.keep) {
+    ET_ROW(streamed_kernel, 4, 8 / F, false);
+  } else if (plan.nt && SAME) {
+    if (plan.waves == 4) ET_ROW(kept_kernel, 4, 16 / F, SAME);
+    else if (plan.waves == 8) ET_ROW(kept_kernel, 8, 16 / F, SAME);
+    else ET_ROW(kept_kernel, 16, 16 / F, SAME);
+  } else {
+    if (plan.waves == 4) ET_ROW(kept_kernel, 4, 16 / F, false);
+    else if (plan.waves == 8) ET_ROW(kept_kernel, 8, 16 / F, false);
+    else ET_ROW(kept_kernel, 16, 16 / F, false);
   }
 #undef ET_ROW
 }

@@ -25,14 +25,14 @@ __global__ __launch_bounds__(256) void count_kernel(RowArgs a, int* __restrict__
   if (threadIdx.x == 0) counts[blockIdx.x] = n;
 }
 
-// Adds the lines of partial sums: out = scale * column 0, more[i - 1] = scale * column i.  of: divide by this column instead (zero over zero is zero)
-template <int COLS, int OF>
-__global__ __launch_bounds__(1024) void finish_kernel(const double* __restrict__ parts, int lines, double scale, float* __restrict__ out, float* __restrict__ more, int n_more) {
-  __shared__ double red[16][COLS];
+// Adds the lines of partial sums, by a workgroup: out = scale * column 0, more[i - 1] = scale * column i.  OF >= 0: divided by that column instead (zero over zero is zero)
+template <int THREADS, int COLS, int OF>
+__device__ __forceinline__ void finish(const double* __restrict__ parts, int lines, double scale, float* __restrict__ out, float* __restrict__ more, int n_more) {
+  __shared__ double red[THREADS / 64][COLS];
   double v[COLS];
 #pragma unroll
   for (int i = 0; i < COLS; i++) v[i] = 0;
-  for (int l = threadIdx.x; l < lines; l += 1024)
+  for (int l = threadIdx.x; l < lines; l += THREADS)
 #pragma unroll
     for (int i = 0; i < COLS; i++) v[i] += parts[(size_t)COLS * l + i];
 #pragma unroll
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(1024) void finish_kernel(const double* __restrict__
   __syncthreads();
   if (threadIdx.x >= COLS) return;
   double n = 0, s = 0;
-  for (int w = 0; w < 16; w++) {
+  for (int w = 0; w < THREADS / 64; w++) {
     s += red[w][threadIdx.x];
     if (OF >= 0) n += red[w][OF < 0 ? 0 : OF];
   }
@@ -52,12 +52,127 @@ __global__ __launch_bounds__(1024) void finish_kernel(const double* __restrict__
   if (threadIdx.x == 0) *out = (float)(s * scale);
   else if (more && (int)threadIdx.x <= n_more) more[threadIdx.x - 1] = (float)(s * scale);
 }
+template <int THREADS, int COLS, int OF>
+__global__ __launch_bounds__(THREADS) void finish_kernel(const double* __restrict__ parts, int lines, double scale, float* __restrict__ out, float* __restrict__ more,
+                                                         int n_more) {
+  finish<THREADS, COLS, OF>(parts, lines, scale, out, more, n_more);
+}
+template <int COLS, int OF>
+void finish_launch(hipStream_t s, const double* parts, int lines, double scale, float* out, float* more, int n_more) {
+  if (lines <= 512) hipLaunchKernelGGL((finish_kernel<256, COLS, OF>), dim3(1), dim3(256), 0, s, parts, lines, scale, out, more, n_more);
+  else hipLaunchKernelGGL((finish_kernel<1024, COLS, OF>), dim3(1), dim3(1024), 0, s, parts, lines, scale, out, more, n_more);
+}
 
 // ---- preference
-__device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
+struct PairArgs {
+  const float* ref;
+  double beta, eps, per_pair;
+  float* logp;
+};
+__device__ __forceinline__ double softplus(double x) { return x == INFINITY ? x : (x > 0 ? x : 0.0 * x) + log1p_d(exp_d(-fabs(x))); }
+// of a pair's margin: the factor of its gradient, and its loss
+__device__ __forceinline__ float pair_factor(const PairArgs& q, double z) {
+  const double up = 1.0 / (1.0 + exp_d(-z)), down = 1.0 / (1.0 + exp_d(z));
+  return (float)(((q.eps != 0 ? q.eps * up : 0.0) - (q.eps != 1 ? (1 - q.eps) * down : 0.0)) * q.beta * q.per_pair);
+}
+__device__ __forceinline__ double pair_loss(const PairArgs& q, double z) {
+  return (q.eps != 1 ? (1 - q.eps) * softplus(-z) : 0.0) + (q.eps != 0 ? q.eps * softplus(z) : 0.0);
+}
+__device__ __forceinline__ double pair_margin(const PairArgs& q, int pair, double chosen, double other) {
+  return q.beta * ((chosen - (q.ref ? (double)q.ref[2 * pair] : 0.0)) - (other - (q.ref ? (double)q.ref[2 * pair + 1] : 0.0)));
+}
 
-__global__ __launch_bounds__(256) void pair_kernel(Sequences seq, SeqRows o, const float* __restrict__ ref, double beta, double eps, double per_pair,
-                                                   float* __restrict__ logp, double* __restrict__ parts) {
+// Pairs of single rows, a wave each: both rows stay in registers
+constexpr int PAIR_VECS = 4;
+bool pair_rows_fit(int classes, size_t size) { return (int64_t)classes * (int64_t)size <= 64 * 16 * PAIR_VECS; }
+template <typename T, typename G>
+__global__ __launch_bounds__(256) void pair_rows_kernel(RowArgs a, PairArgs q, double* __restrict__ parts) {
+  constexpr int N = Vec<T>::N, NV = PAIR_VECS;
+  const int lane = threadIdx.x & 63, pair = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (2ll * pair + 1 >= a.rows) return;
+  u32x4 x[2][NV];
+  float xe[2];
+  int at[2];
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    const int r = 2 * pair + i;
+    const T* row = (const T*)a.logits + (long long)r * a.ld;
+    const RowShape<T, 1> s(a.classes, row, lane);
+    at[i] = a.label[r];
+#pragma unroll
+    for (int v = 0; v < NV; v++)
+      if (v < s.mine) x[i][v] = load_vec(row + s.head + (v * 64 + lane) * N);
+    xe[i] = lane < s.edge ? (float)row[s.edge_at(lane)] : -INFINITY;
+  }
+  RowStat stat[2];
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    const T* row = (const T*)a.logits + (2ll * pair + i) * a.ld;
+    const RowShape<T, 1> s(a.classes, row, lane);
+    at[i] = __builtin_amdgcn_readfirstlane(at[i]);
+    stat[i] = {0, 0, 0, 0, 0, 0, 0.f, true};
+    if (a.masked(at[i])) continue;
+    const LabelAt place(s, at[i]);
+    const float xa = (float)row[at[i]];
+    RunPair run;
+    run.start();
+#pragma unroll
+    for (int v = 0; v < NV; v++)
+      if (v < s.mine) {
+        if (v == place.v && lane == place.t) take_out<T>(x[i][v], place.k);
+        float f[N];
+        unpack<T>(x[i][v], f);
+        run.add<false>(f, f);
+      }
+    if (place.v < 0 && lane == place.t) xe[i] = -INFINITY;
+    if (lane < s.edge) {
+      const float f[1] = {xe[i]};
+      run.add<false>(f, f);
+    }
+    run.over_lanes<false, 64>();
+    stat[i] = row_stat(run.x, xa);
+  }
+  const double L0 = stat[0].none ? 0.0 : stat[0].lp, L1 = stat[1].none ? 0.0 : stat[1].lp, z = pair_margin(q, pair, L0, L1);
+  if (lane == 0) {
+    if (q.logp) {
+      q.logp[2 * pair] = (float)L0;
+      q.logp[2 * pair + 1] = (float)L1;
+    }
+    parts[3 * (size_t)pair] = pair_loss(q, z);
+    parts[3 * (size_t)pair + 1] = z;
+    parts[3 * (size_t)pair + 2] = z > 0 ? 1.0 : 0.0;
+  }
+  if (!a.grad) return;
+  const float factor = pair_factor(q, z);
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    const int r = 2 * pair + i;
+    const RowShape<T, 1> s(a.classes, (const T*)a.logits + (long long)r * a.ld, lane);
+    const LabelAt place(s, at[i]);
+    const bool none = stat[i].none;   // (and what a masked row holds is not looked at)
+    const float g = i == 0 ? factor : -factor;
+    const RowGrad b = {stat[i].m, none ? 0.f : (float)(-g * stat[i].inv_s), 0.f, 0.f, none ? 0.f : (float)(g * (stat[i].rest * stat[i].inv_s))};
+    G* const out = (G*)a.grad + (long long)r * a.gld;
+#pragma unroll
+    for (int v = 0; v < NV; v++)
+      if (v < s.mine) {
+        float f[N], d[N];
+        unpack<T>(x[i][v], f);
+        gradient<false>(b, f, f, d);
+#pragma unroll
+        for (int k = 0; k < N; k++) d[k] = none ? 0.f : v == place.v && lane == place.t && k == place.k ? b.own : d[k];
+        store_vec(out + s.head + (v * 64 + lane) * N, d);
+      }
+    if (lane < s.edge) {
+      const float f[1] = {xe[i]};
+      float d[1];
+      gradient<false>(b, f, f, d);
+      out[s.edge_at(lane)] = (G)(none ? 0.f : place.v == -1 && lane == place.t ? b.own : d[0]);
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void pair_kernel(Sequences seq, SeqRows o, PairArgs q, double* __restrict__ parts) {
   __shared__ double red[4];
   const int pair = blockIdx.x;
   double L[2];
@@ -67,33 +182,36 @@ __global__ __launch_bounds__(256) void pair_kernel(Sequences seq, SeqRows o, con
     double v = 0;
     for (int r = begin + (int)threadIdx.x; r < end; r += 256) v += o.lp[r];
     L[i] = block_sum_d(v, red);
-    if (logp && threadIdx.x == 0) logp[2 * pair + i] = (float)L[i];
+    if (q.logp && threadIdx.x == 0) q.logp[2 * pair + i] = (float)L[i];
   }
-  const double z = beta * ((L[0] - (ref ? (double)ref[2 * pair] : 0.0)) - (L[1] - (ref ? (double)ref[2 * pair + 1] : 0.0)));
-  const double up = 1.0 / (1.0 + exp(-z)), down = 1.0 / (1.0 + exp(z));
-  const double dz = (eps != 0 ? eps * up : 0.0) - (eps != 1 ? (1 - eps) * down : 0.0);
-  const float g = (float)(dz * beta * per_pair);
+  const double z = pair_margin(q, pair, L[0], L[1]);
+  const float g = pair_factor(q, z);
 #pragma unroll
   for (int i = 0; i < 2; i++) {
     const int begin = seq.at(2 * pair + i), end = seq.at(2 * pair + i + 1);
     for (int r = begin + (int)threadIdx.x; r < end; r += 256) o.g[r] = i == 0 ? g : -g;
   }
   if (threadIdx.x == 0) {
-    parts[3 * pair] = (eps != 1 ? (1 - eps) * softplus(-z) : 0.0) + (eps != 0 ? eps * softplus(z) : 0.0);
+    parts[3 * pair] = pair_loss(q, z);
     parts[3 * pair + 1] = z;
     parts[3 * pair + 2] = z > 0 ? 1.0 : 0.0;
   }
 }
 
-// The gradient once the factors are known: nothing but a map of the logits.  A wave takes GRAD_VECS vectors a lane of a row at a time.
+// The gradient once the factors are known: nothing but a map of the logits.  A wave takes GRAD_VECS vectors a lane of a row at a time.  The last workgroup adds up the pairs.
 constexpr int GRAD_VECS = 8;
 template <typename T, typename G>
-__global__ __launch_bounds__(256) void pair_grad_kernel(RowArgs a, Sequences seq, SeqRows o) {
+__global__ __launch_bounds__(256) void pair_grad_kernel(RowArgs a, Sequences seq, SeqRows o, const double* __restrict__ parts, float* __restrict__ loss,
+                                                        float* __restrict__ stats) {
+  if (blockIdx.x == gridDim.x - 1) {
+    finish<256, 3, -1>(parts, seq.n / 2, 2.0 / seq.n, loss, stats, 2);
+    return;
+  }
   constexpr int N = Vec<T>::N, PIECE = 64 * N * GRAD_VECS;
   const int begin = seq.at(0), end = seq.at(seq.n), lane = threadIdx.x & 63;
   const int C = a.classes, Cv = C - C % N, pieces = (C - 1) / PIECE + 1;
   const long long tasks = (long long)(end - begin) * pieces;
-  for (long long task = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); task < tasks; task += gridDim.x * 4ll) {
+  for (long long task = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); task < tasks; task += (gridDim.x - 1) * 4ll) {
     const int r = begin + (int)(task / pieces), j0 = (int)(task % pieces) * PIECE;
     G* const out = (G*)a.grad + (long long)r * a.gld;
     const T* x = (const T*)a.logits + (long long)r * a.ld;
@@ -181,7 +299,7 @@ int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_
   int* counts = (int*)workspace_dev;
   c.counts = counts;
   c.parts = (double*)(counts + MAX_COUNTS);
-  const et::rows::RowPlan plan = et::rows::row_plan(classes, type_size(dtype), c.p.ref != nullptr, grad_dev != nullptr, device_cus(on.dev));
+  const et::rows::RowPlan plan = et::rows::row_plan(rows, classes, type_size(dtype), c.p.ref != nullptr, grad_dev != nullptr, false, device_cus(on.dev));
   const int grid = et::rows::row_grid(rows, plan);
   if (grad_dev && !p->weight_dev && rows > et::rows::COUNT_ROWS) {
     c.n_counts = std::min(MAX_COUNTS, rows / 4096);
@@ -192,9 +310,9 @@ int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_
   // (without a gradient rows have the weight 1 as they are added up)
   const int lines = grid * plan.teams();
   if (!grad_dev && !p->weight_dev)
-    hipLaunchKernelGGL((et::rows::finish_kernel<et::rows::COLUMNS, 4>), dim3(1), dim3(1024), 0, s, c.parts, lines, 1.0, loss_dev, p->stats_dev, 3);
+    et::rows::finish_launch<et::rows::COLUMNS, 4>(s, c.parts, lines, 1.0, loss_dev, p->stats_dev, 3);
   else
-    hipLaunchKernelGGL((et::rows::finish_kernel<et::rows::COLUMNS, -1>), dim3(1), dim3(1024), 0, s, c.parts, lines, 1.0, loss_dev, p->stats_dev, 3);
+    et::rows::finish_launch<et::rows::COLUMNS, -1>(s, c.parts, lines, 1.0, loss_dev, p->stats_dev, 3);
   return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
 }
 
@@ -215,30 +333,43 @@ int et_preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void*
   et::rows::RowCall c = {};
   c.a = {logits_dev, row_stride, label_dev, grad_dev, grad_stride, rows, classes};
   c.seq = {p->offsets_dev, rows, 2 * pairs};
+  const et::rows::PairArgs q = {p->ref_logp_dev, (double)p->beta, (double)p->label_smoothing, 1.0 / pairs, p->logp_dev};
+  if (!p->offsets_dev && et::rows::pair_rows_fit(classes, type_size(dtype))) {
+    double* parts = (double*)workspace_dev;
+#define ET_PAIR_ROWS(T, G) hipLaunchKernelGGL((et::rows::pair_rows_kernel<T, G>), dim3((pairs + 3) / 4), dim3(256), 0, s, c.a, q, parts)
+    if (dtype == ET_BF16) {
+      if (grad_dtype == ET_BF16) ET_PAIR_ROWS(bf16, bf16); else ET_PAIR_ROWS(bf16, float);
+    } else {
+      if (grad_dtype == ET_BF16) ET_PAIR_ROWS(float, bf16); else ET_PAIR_ROWS(float, float);
+    }
+#undef ET_PAIR_ROWS
+    et::rows::finish_launch<3, -1>(s, parts, pairs, 1.0 / pairs, loss_dev, p->stats_dev, 2);
+    return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
+  }
   c.o.lp = (double*)workspace_dev;
   double* parts = c.o.lp + rows;
   c.o.m = (float*)(parts + 3 * (size_t)pairs);
   c.o.s = c.o.m + rows;
   c.o.rest = c.o.s + rows;
   c.o.g = c.o.rest + rows;
-  const et::rows::RowPlan plan = et::rows::row_plan(classes, type_size(dtype), false, false, device_cus(on.dev));
+  const et::rows::RowPlan plan = et::rows::row_plan(rows, classes, type_size(dtype), false, false, grad_dev != nullptr, device_cus(on.dev));
   const int grid = plan.waves == 1 ? et::rows::row_grid(rows, plan) : std::min(rows, 1 << 20);
   if (dtype == ET_BF16) et::rows::rows_of_statistics<bf16>(plan, grid, s, c);
   else et::rows::rows_of_statistics<float>(plan, grid, s, c);
-  hipLaunchKernelGGL(et::rows::pair_kernel, dim3(pairs), dim3(256), 0, s, c.seq, c.o, p->ref_logp_dev, (double)p->beta, (double)p->label_smoothing, 1.0 / pairs,
-                     p->logp_dev, parts);
+  hipLaunchKernelGGL(et::rows::pair_kernel, dim3(pairs), dim3(256), 0, s, c.seq, c.o, q, parts);
   if (grad_dev) {
     const int64_t piece = 64 * et::rows::GRAD_VECS * (16 / (int64_t)type_size(dtype)), tasks = rows * ((classes + piece - 1) / piece);
     const int groups = (int)std::min<int64_t>((tasks + 3) / 4, 1 << 20);
-#define ET_PAIR_GRAD(T, G) hipLaunchKernelGGL((et::rows::pair_grad_kernel<T, G>), dim3(groups), dim3(256), 0, s, c.a, c.seq, c.o)
+#define ET_PAIR_GRAD(T, G) hipLaunchKernelGGL((et::rows::pair_grad_kernel<T, G>), dim3(groups + 1), dim3(256), 0, s, c.a, c.seq, c.o, parts, loss_dev, p->stats_dev)
     if (dtype == ET_BF16) {
       if (grad_dtype == ET_BF16) ET_PAIR_GRAD(bf16, bf16); else ET_PAIR_GRAD(bf16, float);
     } else {
       if (grad_dtype == ET_BF16) ET_PAIR_GRAD(float, bf16); else ET_PAIR_GRAD(float, float);
     }
 #undef ET_PAIR_GRAD
+    return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
   }
-  hipLaunchKernelGGL((et::rows::finish_kernel<3, -1>), dim3(1), dim3(1024), 0, s, parts, pairs, 1.0 / pairs, loss_dev, p->stats_dev, 2);
+  et::rows::finish_launch<3, -1>(s, parts, pairs, 1.0 / pairs, loss_dev, p->stats_dev, 2);
   return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
 }
 
