@@ -325,7 +325,8 @@ def _bound(s):
                                          at(loss)), out
     ws = room(et.et_preference_loss_ws_bytes(rows, s["pairs"]))
     out["stats"], out["logp"] = f32(2), f32(2 * s["pairs"])
-    p = et.make_preference(at(s["offsets"]), ref_logp=at(s["ref"]), beta=BETA, label_smoothing=s["smoothing"], logp=at(out["logp"]), stats=at(out["stats"]))
+    # (every row a sequence: the call takes that without offsets)
+    p = et.make_preference(at(s["offsets"]) if s["longest"] else 0, ref_logp=at(s["ref"]), beta=BETA, label_smoothing=s["smoothing"], logp=at(out["logp"]), stats=at(out["stats"]))
     return lambda: et.et_preference_loss(rows, s["pairs"], C, at(s["logits"]), dtype, ld, at(s["label"]), p, at(grad), dtype, ld, at(ws), ws.numel(),
                                          stream, at(loss)), out
 
