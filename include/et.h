@@ -357,6 +357,31 @@ int et_grad_clip(int32_t n, const void* const* grad_dev, void* const* out_dev, c
 int et_grad_scale(int32_t n, const void* const* grad_dev, void* const* out_dev, const uint64_t* numel, int32_t dtype, const float* norm_dev, float max_norm,
                   void* hip_stream);
 
+/* The step with another objective than the mean cross-entropy, and with the gradients of the selected tensors clipped by their common norm.
+ *   objective ET_LOSS_XENT: as et_train_step; policy, preference unused.
+ *   ET_LOSS_POLICY: et_policy_loss on the logits of the batch, y_dev the actions (one outside [0, classes) masks its sample);
+ *     policy->ref_logits_dev is float32.
+ *   ET_LOSS_PREFERENCE: et_preference_loss, sample 2p preferred over sample 2p + 1 with the labels in y_dev; the batch must be even and preference->offsets_dev NULL.
+ * max_norm > 0: the update takes gradient * c, c as in et_grad_clip with the norm over the selected tensors; a norm that is not finite skips the update, and weights and state keep
+ * their bytes.  grad_dev keeps the gradients as computed.  max_norm == 0: no clipping.  norm_dev (device, or NULL) receives the norm; 0 of an empty mask.
+ * workspace_dev: as for the stand-alone operators, at least et_step_workspace_bytes() bytes; may be NULL with ET_LOSS_XENT.  The structs are host memory, read before the call
+ * returns; their device pointers are used on the stream.  options == NULL: et_train_step. */
+#define ET_LOSS_XENT 0
+#define ET_LOSS_POLICY 1
+#define ET_LOSS_PREFERENCE 2
+typedef struct {
+  int32_t objective;
+  const et_policy* policy;
+  const et_preference* preference;
+  float max_norm;
+  float* norm_dev;
+  void* workspace_dev;
+  size_t workspace_bytes;
+} et_step_options;
+size_t et_step_workspace_bytes(const et_ctx* ctx);
+int et_train_step_with(et_ctx* ctx, const void* x_dev, const int32_t* y_dev, const uint8_t* mask_host /*[N]*/, const et_opt* opt,
+                       const et_step_options* options, float* loss_host);
+
 /* Counters of the last et_train_step/et_importance call on this context: kernels launched in
  * the forward pass, in the backward pass and in the optimizer update. */
 int et_last_launch_counts(const et_ctx* ctx, int32_t* forward, int32_t* backward, int32_t* update);

@@ -17,6 +17,7 @@ ET_OK, ET_INFEASIBLE, ET_EINVAL, ET_ENOMEM, ET_EHIP, ET_ENAN, ET_ESTATE = 0, 1, 
 ET_MLP, ET_VIT, ET_RESNET, ET_VGG, ET_MOBILENET = 0, 1, 2, 3, 4
 ET_F32, ET_BF16 = 0, 1
 ET_ADAM, ET_SGDW = 0, 1
+ET_LOSS_XENT, ET_LOSS_POLICY, ET_LOSS_PREFERENCE = 0, 1, 2
 ET_MAX_MLP_LAYERS = 16
 ET_MAX_STAGES = 8
 
@@ -47,6 +48,11 @@ class et_preference(C.Structure):
                 ("logp_dev", C.c_void_p), ("stats_dev", C.c_void_p)]
 
 
+class et_step_options(C.Structure):
+    _fields_ = [("objective", C.c_int32), ("policy", C.POINTER(et_policy)), ("preference", C.POINTER(et_preference)), ("max_norm", C.c_float),
+                ("norm_dev", C.c_void_p), ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 class EtError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -74,6 +80,8 @@ def _load():
         "et_select": (C.c_int, [i32, C.POINTER(C.c_double), C.POINTER(u64), C.POINTER(u64), u64, C.c_uint32,
                                 C.c_uint32, C.POINTER(C.c_uint8), C.POINTER(u64)]),
         "et_train_step": (C.c_int, [vp, vp, vp, C.POINTER(C.c_uint8), C.POINTER(et_opt), C.POINTER(C.c_float)]),
+        "et_step_workspace_bytes": (C.c_size_t, [vp]),
+        "et_train_step_with": (C.c_int, [vp, vp, vp, C.POINTER(C.c_uint8), C.POINTER(et_opt), C.POINTER(et_step_options), C.POINTER(C.c_float)]),
         "et_policy_loss_ws_bytes": (C.c_size_t, [i32]),
         "et_policy_loss": (C.c_int, [i32, i32, vp, i32, C.c_int64, vp, C.POINTER(et_policy), vp, i32, C.c_int64, vp, C.c_size_t, vp, vp]),
         "et_preference_loss_ws_bytes": (C.c_size_t, [i32, i32]),
@@ -124,6 +132,7 @@ _lib = _load()
 EXPORTS = ["et_create", "et_destroy", "et_num_tensors", "et_tensor_info", "et_workspace_bytes", "et_workspace_min_bytes", "et_state_slots",
            "et_bind", "et_profile", "et_importance", "et_importance_master", "et_importance_reduce_static", "et_select", "et_select_stats", "et_tensor_metric", "et_train_step", "et_last_launch_counts",
            "et_policy_loss", "et_policy_loss_ws_bytes", "et_preference_loss", "et_preference_loss_ws_bytes", "et_grad_norm", "et_grad_norm_ws_bytes", "et_grad_clip", "et_grad_scale",
+           "et_train_step_with", "et_step_workspace_bytes",
            "et_kernel_timing", "et_kernel_timing_read", "et_kernel_timing_overhead", "et_last_hip_error", "et_strerror", "et_debug_gemm_bf16", "et_debug_copy", "et_debug_mfma_peak", "et_debug_conv3x3",
            "et_debug_conv3x3_dw", "et_debug_depthwise3x3", "et_debug_depthwise3x3_ws_floats", "et_debug_affine_back", "et_debug_affine_back_ws_floats", "et_debug_flip3x3", "et_debug_dw_chunks", "et_debug_gemm_tile", "et_debug_gemm_bf16_act", "et_debug_conv3x3_plan", "et_debug_dw_group", "et_debug_conv_first",
            "et_debug_activation", "et_debug_conv3x3_split", "et_debug_attention", "et_debug_attention_long", "et_debug_attention_long_rest", "et_debug_gemm_bf16_colsum",
@@ -312,6 +321,31 @@ def et_train_step(ctx, x_dev, y_dev, mask, opt=None, want_loss=True):
     _check(_lib.et_train_step(ctx, C.c_void_p(x_dev), C.c_void_p(y_dev), m.ctypes.data_as(C.POINTER(C.c_uint8)),
                               C.byref(opt) if opt is not None else None, C.byref(loss) if want_loss else None),
            "et_train_step", ctx=ctx)
+    return loss.value if want_loss else None
+
+
+def et_step_workspace_bytes(ctx):
+    return _lib.et_step_workspace_bytes(ctx)
+
+
+def make_step_options(policy=None, preference=None, max_norm=0.0, norm=0, ws=0, ws_bytes=0):
+    """policy (make_policy) or preference (make_preference) choose the objective, neither the mean cross-entropy; norm, ws: device addresses."""
+    if policy is not None and preference is not None:
+        raise EtError(ET_EINVAL, "make_step_options")
+    o = et_step_options()
+    o.objective = ET_LOSS_POLICY if policy is not None else ET_LOSS_PREFERENCE if preference is not None else ET_LOSS_XENT
+    o.policy = C.pointer(policy) if policy is not None else None
+    o.preference = C.pointer(preference) if preference is not None else None
+    o.max_norm, o.norm_dev, o.workspace_dev, o.workspace_bytes = max_norm, norm, ws, ws_bytes
+    return o
+
+
+def et_train_step_with(ctx, x_dev, y_dev, mask, opt=None, options=None, want_loss=True):
+    m = np.ascontiguousarray(mask, dtype=np.uint8)
+    loss = C.c_float()
+    _check(_lib.et_train_step_with(ctx, C.c_void_p(x_dev), C.c_void_p(y_dev), m.ctypes.data_as(C.POINTER(C.c_uint8)),
+                                   C.byref(opt) if opt is not None else None, C.byref(options) if options is not None else None,
+                                   C.byref(loss) if want_loss else None), "et_train_step_with", ctx=ctx)
     return loss.value if want_loss else None
 
 

@@ -12,6 +12,7 @@
 
 #include "et.h"
 #include "kernels.h"
+#include "op_args.h"
 
 using et::bf16;
 
@@ -167,6 +168,8 @@ struct et_ctx {
   std::vector<et::UpdateSeg> upd_segs_host;
   std::vector<et::TensorSeg> imp_segs_host;
 
+  const et_step_options* step = nullptr;  // of the call that runs (null: the mean cross-entropy)
+
   // launch accounting and profiling
   int32_t launches[4] = {0, 0, 0, 0};
   int cur_phase = PH_FWD;
@@ -299,6 +302,24 @@ inline int colsum_dw(et_ctx* c, int tensor, const bf16* d, const float* d32, lon
   Region r(c, PH_DW, tensor);
   float* part = sum_job(c, tensor, parts, cols);
   ET_K(1, et::colsum_part(d, d32, d_stride, h, h_stride, mean, rstd, stat_stride, part, rows, cols, c->stream));
+  return ET_OK;
+}
+
+// the loss of the batch in c->loss, and its gradient in c->dlogits and, for a model that has it, as rounded in c->dl16 (rows of ld16, zero padded)
+inline int loss_and_gradient(et_ctx* c, const int32_t* y, int B, int C, int ld16) {
+  const et_step_options* o = c->step;
+  if (!o || o->objective == ET_LOSS_XENT) {
+    ET_K(2, et::xent(c->logits, y, B, C, c->loss, c->dlogits, c->dl16, ld16, c->stream));
+    return ET_OK;
+  }
+  int n = 0;
+  const int rc = o->objective == ET_LOSS_POLICY
+                     ? et_op::policy_loss(B, C, c->logits, ET_F32, C, y, o->policy, c->dlogits, ET_F32, C, o->workspace_dev, o->workspace_bytes, c->stream, c->loss, false, &n)
+                     : et_op::preference_loss(B, B / 2, C, c->logits, ET_F32, C, y, o->preference, c->dlogits, ET_F32, C, o->workspace_dev, o->workspace_bytes, c->stream,
+                                              c->loss, false, &n);
+  if (rc != ET_OK) return rc;
+  c->launches[c->cur_phase] += n;
+  if (c->dl16) ET_K(1, et::round_rows(c->dlogits, c->dl16, B, C, ld16, c->stream));
   return ET_OK;
 }
 

@@ -149,8 +149,7 @@ int mlp_forward(et_ctx* c, const void* x, const int32_t* y) {
     g.relu_out = i + 1 < L;
     ET_K(1, et::gemm_f32(g, c->stream));
   }
-  ET_K(2, et::xent(c->logits, y, B, d.dims[L], c->loss, c->dlogits, nullptr, d.dims[L], c->stream));
-  return ET_OK;
+  return loss_and_gradient(c, y, B, d.dims[L], d.dims[L]);
 }
 
 int mlp_backward(et_ctx* c, const void* x, const uint8_t* mask) {
@@ -285,8 +284,7 @@ int vit_forward(et_ctx* c, const void* x, const int32_t* y, const uint8_t* mask)
     g.C = c->logits; g.c_f32 = true;
     ET_G(g);
   }
-  ET_K(2, et::xent(c->logits, y, v.B, v.C, c->loss, c->dlogits, c->dl16, v.C8, c->stream));
-  return ET_OK;
+  return loss_and_gradient(c, y, v.B, v.C, v.C8);
 }
 
 // part: where the fused core leaves the partial column sums of dqkv (the bias of the product in front of it), or null
@@ -605,12 +603,9 @@ int run_backward(et_ctx* c, const void* x, const uint8_t* mask) {
   return rc == ET_OK ? sums_finish(c) : rc;
 }
 
-int run_update(et_ctx* c, const uint8_t* mask, const et_opt* opt, bool dry) {
+// the chunks of the selected tensors, listed on the device; rebuilt only when the mask changes
+int list_selected(et_ctx* c, const uint8_t* mask) {
   const size_t N = c->tensors.size();
-  if (c->state.empty()) return ET_ESTATE;
-  if (opt->kind != ET_ADAM && opt->kind != ET_SGDW) return ET_EINVAL;
-  if (opt->kind == ET_ADAM && opt->step < 1) return ET_EINVAL;
-  // the chunks of the selected tensors, listed on the device; rebuilt only when the mask changes
   std::vector<uint8_t> norm(N);
   for (size_t i = 0; i < N; i++) norm[i] = mask[i] ? 1 : 0;
   if (c->upd_mask != norm) {
@@ -623,6 +618,17 @@ int run_update(et_ctx* c, const uint8_t* mask, const et_opt* opt, bool dry) {
       ET_HIP(hipMemcpyAsync(c->upd_selected_dev, c->upd_selected.data(), sizeof(uint32_t) * c->upd_selected.size(),
                             hipMemcpyHostToDevice, c->stream));
   }
+  return ET_OK;
+}
+
+// norm_dev, max_norm: as for et::masked_update
+int run_update(et_ctx* c, const uint8_t* mask, const et_opt* opt, bool dry, const float* norm_dev = nullptr, float max_norm = 0.f) {
+  const size_t N = c->tensors.size();
+  if (c->state.empty()) return ET_ESTATE;
+  if (opt->kind != ET_ADAM && opt->kind != ET_SGDW) return ET_EINVAL;
+  if (opt->kind == ET_ADAM && opt->step < 1) return ET_EINVAL;
+  const int rc = list_selected(c, mask);
+  if (rc != ET_OK) return rc;
   if (c->upd_selected.empty()) return ET_OK;
   et::OptParams p;
   p.kind = opt->kind == ET_ADAM ? 0 : 1;
@@ -638,7 +644,7 @@ int run_update(et_ctx* c, const uint8_t* mask, const et_opt* opt, bool dry) {
   // bytes per selected element: read g + fp32 weight + moments, write fp32 weight + moments (+ bf16 copy)
   const double per_elem = (opt->kind == ET_ADAM ? 28.0 : 20.0) + (c->bf16_model ? 2.0 : 0.0);
   KernelTimer kt(c, 4, sel_elems * per_elem);
-  ET_K(1, et::masked_update(c->upd_segs_dev, c->upd_selected_dev, (int)c->upd_selected.size(), c->bf16_model, p, c->stream));
+  ET_K(1, et::masked_update(c->upd_segs_dev, c->upd_selected_dev, (int)c->upd_selected.size(), c->bf16_model, p, c->stream, norm_dev, max_norm));
   return ET_OK;
 }
 
@@ -801,16 +807,55 @@ int et_bind(et_ctx* c, void* const* w_dev, void* const* opt_state_dev, void* con
 
 int et_train_step(et_ctx* c, const void* x_dev, const int32_t* y_dev, const uint8_t* mask_host, const et_opt* opt,
                   float* loss_host) {
+  return et_train_step_with(c, x_dev, y_dev, mask_host, opt, nullptr, loss_host);
+}
+
+size_t et_step_workspace_bytes(const et_ctx* c) {
+  if (!c) return 0;
+  return std::max(et_policy_loss_ws_bytes(c->desc.batch), et_preference_loss_ws_bytes(c->desc.batch, std::max(1, c->desc.batch / 2)));
+}
+
+namespace {
+int train_step(et_ctx* c, const void* x_dev, const int32_t* y_dev, const uint8_t* mask_host, const et_opt* opt, const et_step_options* o, float* loss_host) {
   if (!c || !x_dev || !y_dev || !mask_host) return ET_EINVAL;
   if (!c->bound) return ET_ESTATE;
   if (reinterpret_cast<uintptr_t>(x_dev) & 15) return ET_EINVAL;
+  if (o) {
+    // (what would be refused behind the forward pass is refused in front of it)
+    if (!(o->max_norm >= 0) || (reinterpret_cast<uintptr_t>(o->norm_dev) & 3)) return ET_EINVAL;
+    const int B = c->desc.batch, C = c->desc.kind == ET_MLP ? c->desc.dims[c->desc.n_layers] : c->desc.classes;
+    int rc = ET_OK;
+    if (o->objective == ET_LOSS_POLICY) {
+      rc = et_op::policy_loss(B, C, c->logits, ET_F32, C, y_dev, o->policy, c->dlogits, ET_F32, C, o->workspace_dev, o->workspace_bytes, c->stream, c->loss, true, nullptr);
+    } else if (o->objective == ET_LOSS_PREFERENCE) {
+      if (B % 2 || !o->preference || o->preference->offsets_dev) return ET_EINVAL;
+      rc = et_op::preference_loss(B, B / 2, C, c->logits, ET_F32, C, y_dev, o->preference, c->dlogits, ET_F32, C, o->workspace_dev, o->workspace_bytes, c->stream, c->loss,
+                                  true, nullptr);
+    } else if (o->objective != ET_LOSS_XENT) {
+      return ET_EINVAL;
+    }
+    if (rc != ET_OK) return rc;
+  }
   c->launches[0] = c->launches[1] = c->launches[2] = c->launches[3] = 0;
+  c->step = o;
   int rc = run_forward(c, x_dev, y_dev, mask_host);
+  c->step = nullptr;
   if (rc != ET_OK) return rc;
   rc = run_backward(c, x_dev, mask_host);
   if (rc != ET_OK) return rc;
+  const float* norm = nullptr;
+  if (o && (o->max_norm > 0 || o->norm_dev)) {
+    rc = list_selected(c, mask_host);
+    if (rc != ET_OK) return rc;
+    // (the tables of the importance, which no step uses, hold the chunks' sums)
+    float* at = o->norm_dev ? o->norm_dev : (float*)c->imp_out_dev;
+    const int n = (int)c->upd_selected.size();
+    c->cur_phase = PH_UPD;
+    ET_K(n ? 2 : 1, et::selected_norm(c->upd_segs_dev, c->upd_selected_dev, n, c->imp_partial_dev, at, c->stream));
+    if (o->max_norm > 0) norm = at;
+  }
   if (opt) {
-    rc = run_update(c, mask_host, opt, false);
+    rc = run_update(c, mask_host, opt, false, norm, o ? o->max_norm : 0.f);
     if (rc != ET_OK) return rc;
   }
   if (loss_host) {
@@ -818,6 +863,18 @@ int et_train_step(et_ctx* c, const void* x_dev, const int32_t* y_dev, const uint
     ET_HIP(hipStreamSynchronize(c->stream));
   }
   return ET_OK;
+}
+
+}  // namespace
+
+int et_train_step_with(et_ctx* c, const void* x_dev, const int32_t* y_dev, const uint8_t* mask_host, const et_opt* opt, const et_step_options* options,
+                       float* loss_host) {
+  try {
+    return train_step(c, x_dev, y_dev, mask_host, opt, options, loss_host);
+  } catch (const std::bad_alloc&) {
+    c->step = nullptr;
+    return ET_ENOMEM;
+  }
 }
 
 int et_last_launch_counts(const et_ctx* c, int32_t* forward, int32_t* backward, int32_t* update) {

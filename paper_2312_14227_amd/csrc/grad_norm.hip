@@ -82,17 +82,14 @@ __device__ __forceinline__ double block_sum_d(double v, double* red) {
 
 constexpr int VECS = 8;   // of a thread, on the way at once
 
-template <typename T>
-__global__ __launch_bounds__(256) void squares_kernel(Tensors<NORM_BATCH> t, double* __restrict__ part, uint32_t* __restrict__ begin) {
-  __shared__ double red[4];
-  const uint32_t c = t.begin[0] + blockIdx.x;
-  const int k = tensor_of(t, c);
-  const Piece<T> p = piece_of<T>(t, k, c);
+// a thread's part of a chunk's squares
+template <typename T, typename LOAD>
+__device__ __forceinline__ double squares_of(const Piece<T>& p, LOAD load) {
   double s0 = 0, s1 = 0;
   for (int v0 = threadIdx.x; v0 < p.vecs; v0 += 256 * VECS) {
     u32x4 v[VECS];
 #pragma unroll
-    for (int i = 0; i < VECS; i++) v[i] = v0 + 256 * i < p.vecs ? __builtin_nontemporal_load(p.vec() + v0 + 256 * i) : u32x4{0, 0, 0, 0};
+    for (int i = 0; i < VECS; i++) v[i] = v0 + 256 * i < p.vecs ? load(p.vec() + v0 + 256 * i) : u32x4{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < VECS; i++)
 #pragma unroll
@@ -106,10 +103,29 @@ __global__ __launch_bounds__(256) void squares_kernel(Tensors<NORM_BATCH> t, dou
     const double a = (double)(float)p.g[p.edge_at(threadIdx.x)];
     s0 = fma(a, a, s0);
   }
-  const double s = block_sum_d<4>(s0 + s1, red);
+  return s0 + s1;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void squares_kernel(Tensors<NORM_BATCH> t, uint32_t cached_from, double* __restrict__ part, uint32_t* __restrict__ begin) {
+  __shared__ double red[4];
+  const uint32_t c = t.begin[0] + blockIdx.x;
+  const int k = tensor_of(t, c);
+  const Piece<T> p = piece_of<T>(t, k, c);
+  const double mine = c < cached_from ? squares_of(p, [](const u32x4* at) { return __builtin_nontemporal_load(at); }) : squares_of(p, [](const u32x4* at) { return *at; });
+  const double s = block_sum_d<4>(mine, red);
   if (threadIdx.x == 0 && p.n > 0) part[c] = s;   // (a launch of empty tensors has a workgroup, but no chunk)
   // what the next launch needs of the table
   for (int i = blockIdx.x * 256 + threadIdx.x; i < t.n; i += gridDim.x * 256) begin[t.first + i] = t.begin[i];
+}
+
+// the same over chunks of a context's table (16-byte aligned, float32)
+__global__ __launch_bounds__(256) void selected_squares_kernel(const UpdateSeg* __restrict__ segs, const uint32_t* __restrict__ selected, double* __restrict__ part) {
+  __shared__ double red[4];
+  const UpdateSeg sg = segs[selected[blockIdx.x]];
+  const Piece<float> p(sg.g, (int)sg.n);
+  const double s = block_sum_d<4>(squares_of(p, [](const u32x4* at) { return *at; }), red);   // (the update reads them again)
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
 // workgroup 0: the norm of all; k + 1: of tensor k
@@ -123,10 +139,6 @@ __global__ __launch_bounds__(1024) void norms_kernel(const double* __restrict__ 
   for (uint32_t c = from + threadIdx.x; c < to; c += 1024) s += part[c];
   s = block_sum_d<16>(s, red);
   if (threadIdx.x == 0) (k < 0 ? norm[0] : tensor_norm[k]) = (float)sqrt(s);
-}
-
-__device__ __forceinline__ float clip_scale(float norm, float max_norm) {
-  return isfinite(norm) && norm > max_norm ? (float)((double)max_norm / (double)norm) : 1.f;
 }
 
 template <typename T>
@@ -167,6 +179,14 @@ __global__ __launch_bounds__(256) void scale_kernel(ScaleTensors t, const float*
 }
 
 }  // namespace
+
+hipError_t selected_norm(const UpdateSeg* segs_dev, const uint32_t* selected_dev, int n_selected, double* part_dev, float* norm_dev, hipStream_t s) {
+  if (n_selected < 0 || !part_dev || !norm_dev) return hipErrorInvalidValue;
+  if (n_selected > 0) hipLaunchKernelGGL(selected_squares_kernel, dim3(n_selected), dim3(256), 0, s, segs_dev, selected_dev, part_dev);
+  hipLaunchKernelGGL(norms_kernel, dim3(1), dim3(1024), 0, s, part_dev, nullptr, 0, (uint32_t)n_selected, norm_dev, nullptr);
+  return hipGetLastError();
+}
+
 }  // namespace et
 
 namespace {
@@ -177,6 +197,16 @@ struct Plan {
   uint64_t total = 0, chunks = 0;
   uint32_t chunk = 4096;
 };
+
+// The chunk from which on the norm reads through the caches: what follows a norm, clipping or an update, reads the same gradients, and finds the last 192 MB in the last-level
+// cache (256 MB).  86 million float32 gradients: norm and scaling 169 us, past the caches 185.  Up to 128 MB are read past the caches all the same (60 million bf16:
+// 24 us, through them 26), as is what lies in front of the last 192 MB of more (303 million float32: 188 and 208).
+uint32_t cached_from(const Plan& p, size_t size) {
+  const double bytes = (double)p.total * size;
+  if (bytes <= 128e6) return UINT32_MAX;
+  const uint64_t kept = (uint64_t)(192e6 / ((double)p.chunk * size));
+  return p.chunks > kept ? (uint32_t)(p.chunks - kept) : 0;
+}
 
 // False: a size that no memory holds.  Chunks of 64 KB where there are enough of them, so that a workgroup's beginning and end are a small part of it;
 // smaller ones spread few elements over the chip (200 000 of them: 49 workgroups of 4096, 6.0 us, or 13 of 16384, 7.5); larger ones keep the sums of chunks few.
@@ -223,12 +253,13 @@ void norm_launch(int32_t n, const void* const* grad, const uint64_t* numel, int3
   double* part = (double*)ws;
   uint32_t* begin = (uint32_t*)(part + p.chunks);
   uint32_t next = 0;
+  const uint32_t cached = cached_from(p, type_size(dtype));
   for (int32_t first = 0; first < n; first += et::NORM_BATCH) {
     et::Tensors<et::NORM_BATCH> t;
     fill(&t, n, first, grad, numel, p, &next);
     const uint32_t grid = std::max(1u, next - t.begin[0]);
-    if (dtype == ET_BF16) hipLaunchKernelGGL(et::squares_kernel<bf16>, dim3(grid), dim3(256), 0, s, t, part, begin);
-    else hipLaunchKernelGGL(et::squares_kernel<float>, dim3(grid), dim3(256), 0, s, t, part, begin);
+    if (dtype == ET_BF16) hipLaunchKernelGGL(et::squares_kernel<bf16>, dim3(grid), dim3(256), 0, s, t, cached, part, begin);
+    else hipLaunchKernelGGL(et::squares_kernel<float>, dim3(grid), dim3(256), 0, s, t, cached, part, begin);
   }
   hipLaunchKernelGGL(et::norms_kernel, dim3(tensor_norm ? n + 1 : 1), dim3(1024), 0, s, part, begin, n, (uint32_t)p.chunks, norm, tensor_norm);
 }

@@ -249,6 +249,9 @@ int attention_long_bwd_parts(int B, int T);
 hipError_t xent(const float* logits, const int32_t* y, int B, int C, float* loss, float* dlogits, bf16* dlogits_bf16,
                 int ld16, hipStream_t s);
 
+// the bf16 copy on its own: out [rows][ld], zero padded, of in [rows][cols]
+hipError_t round_rows(const float* in, bf16* out, int rows, int cols, int ld, hipStream_t s);
+
 // ViT embedding: h0[b][0] = cls + pos[0]; h0[b][t] = e[b][t-1] + pos[t]  (e fp32 [B*(T-1)][D])
 hipError_t embed_assemble(const float* e, const bf16* cls, const bf16* pos, float* h0, int B, int T, int D, hipStream_t s);
 // drop the CLS rows: out[b*(T-1)+t-1] = bf16(d[b][t]) for t >= 1
@@ -362,8 +365,16 @@ struct OptParams {
   int dry;        // 1: compute, then store the values that were loaded (timing without side effects)
 };
 // segs_dev lists the chunks of ALL tensors, selected_dev the indices of the n_selected chunks that belong to
-// selected tensors: one workgroup per listed chunk, nothing else is touched
+// selected tensors: one workgroup per listed chunk, nothing else is touched.  norm_dev (nullable): the gradients are multiplied with what clips that norm to
+// max_norm (clip_scale); nothing is updated where it is not finite
 hipError_t masked_update(const UpdateSeg* segs_dev, const uint32_t* selected_dev, int n_selected, bool bf16_weights,
-                         OptParams p, hipStream_t s);
+                         OptParams p, hipStream_t s, const float* norm_dev = nullptr, float max_norm = 0.f);
+// norm of the gradients of the listed chunks (n_selected may be 0); part_dev: n_selected doubles of scratch (two launches)
+hipError_t selected_norm(const UpdateSeg* segs_dev, const uint32_t* selected_dev, int n_selected, double* part_dev, float* norm_dev, hipStream_t s);
+#ifdef __HIPCC__
+__device__ __forceinline__ float clip_scale(float norm, float max_norm) {
+  return isfinite(norm) && norm > max_norm ? (float)((double)max_norm / (double)norm) : 1.f;
+}
+#endif
 
 }  // namespace et

@@ -203,8 +203,7 @@ int mobilenet_forward(et_ctx* c, const void* x, const int32_t* y, const uint8_t*
     g.C = c->logits; g.c_f32 = true;
     ET_G(g);
   }
-  ET_K(2, et::xent(c->logits, y, B, d.classes, c->loss, c->dlogits, c->dl16, d.classes, s));
-  return ET_OK;
+  return loss_and_gradient(c, y, B, d.classes, d.classes);
 }
 
 int mobilenet_backward(et_ctx* c, const void* x, const uint8_t* mask) {

@@ -45,4 +45,10 @@ struct Span {
   bool meets(const Span& o) const { return begin < o.end && o.begin < end; }
 };
 
+// The losses, without and with their launches (row_loss.hip); launches: how many (nullable)
+int policy_loss(int32_t rows, int32_t classes, const void* logits, int32_t dtype, int64_t stride, const int32_t* label, const et_policy* p, void* grad, int32_t grad_dtype,
+                int64_t grad_stride, void* ws, size_t ws_bytes, hipStream_t s, float* loss, bool check_only, int* launches);
+int preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void* logits, int32_t dtype, int64_t stride, const int32_t* label, const et_preference* p, void* grad,
+                    int32_t grad_dtype, int64_t grad_stride, void* ws, size_t ws_bytes, hipStream_t s, float* loss, bool check_only, int* launches);
+
 }  // namespace et_op

@@ -123,9 +123,14 @@ __global__ void importance_stage2(const double* __restrict__ partial, const uint
   if (threadIdx.x == 0) out[k] = s;
 }
 
-template <bool BF16W>
-__global__ __launch_bounds__(256) void masked_update_kernel(const UpdateSeg* __restrict__ segs,
-                                                            const uint32_t* __restrict__ selected, OptParams p) {
+template <bool BF16W, bool CLIP>
+__global__ __launch_bounds__(256) void masked_update_kernel(const UpdateSeg* __restrict__ segs, const uint32_t* __restrict__ selected, OptParams p,
+                                                            const float* __restrict__ norm, float max_norm) {
+  float clip = 1.f;
+  if (CLIP) {
+    if (!isfinite(*norm)) return;
+    clip = clip_scale(*norm, max_norm);
+  }
   const UpdateSeg sg = segs[selected[blockIdx.x >> 2]];
   const float* __restrict__ g = sg.g;
   float* __restrict__ m = sg.m;
@@ -134,6 +139,7 @@ __global__ __launch_bounds__(256) void masked_update_kernel(const UpdateSeg* __r
   bf16* __restrict__ wb = (bf16*)sg.w;
   // one element: returns the new weight, updates the moments in place (unless dry)
   auto one = [&](float gi, float w_old, float& mi, float& vi) -> float {
+    if (CLIP) gi *= clip;
     if (p.kind == 0) {
       const float m_new = p.beta1 * mi + (1.f - p.beta1) * gi;
       const float v_new = p.beta2 * vi + (1.f - p.beta2) * gi * gi;
@@ -225,12 +231,15 @@ hipError_t importance_reduce(const TensorSeg* segs_dev, int n_segs, const uint32
 }
 
 hipError_t masked_update(const UpdateSeg* segs_dev, const uint32_t* selected_dev, int n_selected, bool bf16_weights,
-                         OptParams p, hipStream_t s) {
+                         OptParams p, hipStream_t s, const float* norm_dev, float max_norm) {
   if (n_selected <= 0 || n_selected > 0x1fffffff || !selected_dev) return hipErrorInvalidValue;
-  if (bf16_weights)
-    hipLaunchKernelGGL((masked_update_kernel<true>), dim3(4 * n_selected), dim3(256), 0, s, segs_dev, selected_dev, p);
-  else
-    hipLaunchKernelGGL((masked_update_kernel<false>), dim3(4 * n_selected), dim3(256), 0, s, segs_dev, selected_dev, p);
+#define ET_UPDATE(B, C) hipLaunchKernelGGL((masked_update_kernel<B, C>), dim3(4 * n_selected), dim3(256), 0, s, segs_dev, selected_dev, p, norm_dev, max_norm)
+  if (bf16_weights) {
+    if (norm_dev) ET_UPDATE(true, true); else ET_UPDATE(true, false);
+  } else {
+    if (norm_dev) ET_UPDATE(false, true); else ET_UPDATE(false, false);
+  }
+#undef ET_UPDATE
   return hipGetLastError();
 }
 

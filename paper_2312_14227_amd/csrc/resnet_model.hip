@@ -218,8 +218,7 @@ int resnet_forward(et_ctx* c, const void* x, const int32_t* y, const uint8_t* ma
     g.C = c->logits; g.c_f32 = true;
     ET_G(g);
   }
-  ET_K(2, et::xent(c->logits, y, B, d.classes, c->loss, c->dlogits, c->dl16, round8(d.classes), s));
-  return ET_OK;
+  return loss_and_gradient(c, y, B, d.classes, round8(d.classes));
 }
 
 int resnet_backward(et_ctx* c, const void* x, const uint8_t* mask) {

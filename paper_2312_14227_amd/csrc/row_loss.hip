@@ -270,13 +270,9 @@ int check_rows(int32_t rows, int32_t classes, const void* logits, int32_t dtype,
 
 }  // namespace
 
-extern "C" {
-
-size_t et_policy_loss_ws_bytes(int32_t rows) { return rows < 1 ? 0 : POLICY_WS; }
-
-int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_t dtype, int64_t row_stride, const int32_t* label_dev,
-                   const et_policy* p, void* grad_dev, int32_t grad_dtype, int64_t grad_stride, void* workspace_dev, size_t workspace_bytes,
-                   void* hip_stream, float* loss_dev) {
+int et_op::policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_t dtype, int64_t row_stride, const int32_t* label_dev, const et_policy* p,
+                       void* grad_dev, int32_t grad_dtype, int64_t grad_stride, void* workspace_dev, size_t workspace_bytes, hipStream_t s, float* loss_dev,
+                       bool check_only, int* launches) {
   const int rc = check_rows(rows, classes, logits_dev, dtype, row_stride, label_dev, grad_dev, grad_dtype, grad_stride, workspace_dev, loss_dev);
   if (rc != ET_OK) return rc;
   if (!p || !p->old_logp_dev || !p->advantage_dev || (p->ref_logp_dev && p->ref_logits_dev)) return ET_EINVAL;
@@ -289,7 +285,7 @@ int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_
       return ET_EINVAL;
   }
   if (workspace_bytes < POLICY_WS) return ET_ENOMEM;
-  const hipStream_t s = (hipStream_t)hip_stream;
+  if (check_only) return ET_OK;
   const OnDeviceOf on(s);
   if (!on.ok) return ET_EHIP;
   et::rows::RowCall c = {};
@@ -307,6 +303,7 @@ int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_
   }
   if (dtype == ET_BF16) et::rows::rows_of_policy<bf16>(plan, grid, s, c, grad_dtype == ET_BF16);
   else et::rows::rows_of_policy<float>(plan, grid, s, c, grad_dtype == ET_BF16);
+  if (launches) *launches = 2 + (c.n_counts != 0);
   // (without a gradient rows have the weight 1 as they are added up)
   const int lines = grid * plan.teams();
   if (!grad_dev && !p->weight_dev)
@@ -316,18 +313,16 @@ int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_
   return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
 }
 
-size_t et_preference_loss_ws_bytes(int32_t rows, int32_t pairs) { return rows < 1 || pairs < 1 ? 0 : preference_ws(rows, pairs); }
-
-int et_preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void* logits_dev, int32_t dtype, int64_t row_stride,
-                       const int32_t* label_dev, const et_preference* p, void* grad_dev, int32_t grad_dtype, int64_t grad_stride,
-                       void* workspace_dev, size_t workspace_bytes, void* hip_stream, float* loss_dev) {
+int et_op::preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void* logits_dev, int32_t dtype, int64_t row_stride, const int32_t* label_dev,
+                           const et_preference* p, void* grad_dev, int32_t grad_dtype, int64_t grad_stride, void* workspace_dev, size_t workspace_bytes, hipStream_t s,
+                           float* loss_dev, bool check_only, int* launches) {
   const int rc = check_rows(rows, classes, logits_dev, dtype, row_stride, label_dev, grad_dev, grad_dtype, grad_stride, workspace_dev, loss_dev);
   if (rc != ET_OK) return rc;
   if (!p || pairs < 1 || pairs > (INT32_MAX - 1) / 2 || (!p->offsets_dev && rows != 2 * pairs)) return ET_EINVAL;
   if (!aligned(p->offsets_dev, 4) || !aligned(p->ref_logp_dev, 4) || !aligned(p->logp_dev, 4) || !aligned(p->stats_dev, 4)) return ET_EINVAL;
   if (!(p->beta > 0 && std::isfinite(p->beta) && p->label_smoothing >= 0 && p->label_smoothing <= 1)) return ET_EINVAL;
   if (workspace_bytes < preference_ws(rows, pairs)) return ET_ENOMEM;
-  const hipStream_t s = (hipStream_t)hip_stream;
+  if (check_only) return ET_OK;
   const OnDeviceOf on(s);
   if (!on.ok) return ET_EHIP;
   et::rows::RowCall c = {};
@@ -335,6 +330,7 @@ int et_preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void*
   c.seq = {p->offsets_dev, rows, 2 * pairs};
   const et::rows::PairArgs q = {p->ref_logp_dev, (double)p->beta, (double)p->label_smoothing, 1.0 / pairs, p->logp_dev};
   if (!p->offsets_dev && et::rows::pair_rows_fit(classes, type_size(dtype))) {
+    if (launches) *launches = 2;
     double* parts = (double*)workspace_dev;
 #define ET_PAIR_ROWS(T, G) hipLaunchKernelGGL((et::rows::pair_rows_kernel<T, G>), dim3((pairs + 3) / 4), dim3(256), 0, s, c.a, q, parts)
     if (dtype == ET_BF16) {
@@ -346,6 +342,7 @@ int et_preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void*
     et::rows::finish_launch<3, -1>(s, parts, pairs, 1.0 / pairs, loss_dev, p->stats_dev, 2);
     return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
   }
+  if (launches) *launches = 3;
   c.o.lp = (double*)workspace_dev;
   double* parts = c.o.lp + rows;
   c.o.m = (float*)(parts + 3 * (size_t)pairs);
@@ -371,6 +368,25 @@ int et_preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void*
   }
   et::rows::finish_launch<3, -1>(s, parts, pairs, 1.0 / pairs, loss_dev, p->stats_dev, 2);
   return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
+}
+
+extern "C" {
+
+size_t et_policy_loss_ws_bytes(int32_t rows) { return rows < 1 ? 0 : POLICY_WS; }
+size_t et_preference_loss_ws_bytes(int32_t rows, int32_t pairs) { return rows < 1 || pairs < 1 ? 0 : preference_ws(rows, pairs); }
+
+int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_t dtype, int64_t row_stride, const int32_t* label_dev,
+                   const et_policy* policy, void* grad_dev, int32_t grad_dtype, int64_t grad_stride, void* workspace_dev, size_t workspace_bytes,
+                   void* hip_stream, float* loss_dev) {
+  return et_op::policy_loss(rows, classes, logits_dev, dtype, row_stride, label_dev, policy, grad_dev, grad_dtype, grad_stride, workspace_dev, workspace_bytes,
+                            (hipStream_t)hip_stream, loss_dev, false, nullptr);
+}
+
+int et_preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void* logits_dev, int32_t dtype, int64_t row_stride,
+                       const int32_t* label_dev, const et_preference* preference, void* grad_dev, int32_t grad_dtype, int64_t grad_stride,
+                       void* workspace_dev, size_t workspace_bytes, void* hip_stream, float* loss_dev) {
+  return et_op::preference_loss(rows, pairs, classes, logits_dev, dtype, row_stride, label_dev, preference, grad_dev, grad_dtype, grad_stride, workspace_dev,
+                                workspace_bytes, (hipStream_t)hip_stream, loss_dev, false, nullptr);
 }
 
 }  // extern "C"

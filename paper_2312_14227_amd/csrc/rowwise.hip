@@ -212,6 +212,14 @@ __global__ __launch_bounds__(64) void xent_loss_kernel(const float* __restrict__
   *loss = acc / (float)B;
 }
 
+// out[r][i] = in[r][i] rounded, zeros from cols to ld
+__global__ void round_rows_kernel(const float* __restrict__ in, bf16* __restrict__ out, int rows, int cols, int ld) {
+  const long long i = blockIdx.x * (long long)blockDim.x + threadIdx.x;
+  if (i >= (long long)rows * ld) return;
+  const int r = (int)(i / ld), c = (int)(i % ld);
+  out[i] = (bf16)(c < cols ? in[(long long)r * cols + c] : 0.f);
+}
+
 // ---------------------------------------------------------------------------------------------
 // embedding assembly, CLS-row drop, fill
 // ---------------------------------------------------------------------------------------------
@@ -329,6 +337,12 @@ hipError_t softmax_bwd_rows(const float* dp, const bf16* p, bf16* ds, float scal
                             hipStream_t s) {
   if (rows <= 0 || cols <= 0 || ld < cols) return hipErrorInvalidValue;
   hipLaunchKernelGGL(softmax_bwd_rows_kernel, dim3((rows + 3) / 4), dim3(256), 0, s, dp, p, ds, scale, rows, cols, ld);
+  return hipGetLastError();
+}
+
+hipError_t round_rows(const float* in, bf16* out, int rows, int cols, int ld, hipStream_t s) {
+  if (rows <= 0 || cols <= 0 || ld < cols) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(round_rows_kernel, dim3((unsigned)(((long long)rows * ld + 255) / 256)), dim3(256), 0, s, in, out, rows, cols, ld);
   return hipGetLastError();
 }
 

@@ -185,8 +185,7 @@ int vgg_forward(et_ctx* c, const void* x, const int32_t* y) {
     }
     ET_G(g);
   }
-  ET_K(2, et::xent(c->logits, y, B, d.classes, c->loss, c->dlogits, c->dl16, d.classes, s));
-  return ET_OK;
+  return loss_and_gradient(c, y, B, d.classes, d.classes);
 }
 
 int vgg_backward(et_ctx* c, const void* x, const uint8_t* mask) {

@@ -41,6 +41,7 @@ class Session:
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU: the HIP path has no CPU fallback")
         self.cfg, self.dev = cfg, torch.device(device)
+        self.step_ws = None
         self.stream = torch.cuda.current_stream(self.dev)
         self.ctx = et.et_create(desc_from_config(cfg, batch), self.stream.cuda_stream)
         self.n = et.et_num_tensors(self.ctx)
@@ -91,8 +92,16 @@ class Session:
         return [torch.from_numpy(np.ascontiguousarray(s, dtype=np.float32)).to(self.dev).to(self.wdtype).contiguous()
                 for s in snapshot]
 
-    def train_step(self, xt, yt, mask, opt=None, want_loss=True):
-        return et.et_train_step(self.ctx, xt.data_ptr(), yt.data_ptr(), mask, opt, want_loss)
+    def train_step(self, xt, yt, mask, opt=None, want_loss=True, *, policy=None, preference=None, max_norm=0.0, norm=None):
+        """policy (binding.make_policy) or preference (binding.make_preference): the objective instead of the mean cross-entropy; max_norm: clip the selected
+        tensors' gradients in the update; norm: a float32 device tensor that receives their norm."""
+        if policy is None and preference is None and not max_norm and norm is None:
+            return et.et_train_step(self.ctx, xt.data_ptr(), yt.data_ptr(), mask, opt, want_loss)
+        if self.step_ws is None and (policy is not None or preference is not None):
+            self.step_ws = torch.empty(et.et_step_workspace_bytes(self.ctx), dtype=torch.uint8, device=self.dev)
+        options = et.make_step_options(policy, preference, max_norm, norm.data_ptr() if norm is not None else 0,
+                                       self.step_ws.data_ptr() if self.step_ws is not None else 0, self.step_ws.numel() if self.step_ws is not None else 0)
+        return et.et_train_step_with(self.ctx, xt.data_ptr(), yt.data_ptr(), mask, opt, options, want_loss)
 
     def importance(self, xt, yt, snap):
         """snap: list of device tensors in the model's storage type (e.g. clones of self.w)."""
