@@ -338,10 +338,8 @@ constexpr int MAX_GRID = 4096;    // workgroups of the row kernels
 constexpr int COLUMNS = 5;        // sums over rows: loss, surrogate, divergence, clipped; unmasked rows
 constexpr int COUNT_ROWS = 8192;  // rows that a workgroup counts by itself
 
-// unmasked rows among [begin, end), by all threads of a workgroup; red: one entry for each wave
-__device__ __forceinline__ int count_rows(const RowArgs& a, int begin, int end, int* red) {
-  int n = 0;
-  for (int r = begin + (int)threadIdx.x; r < end; r += blockDim.x) n += a.masked(a.label[r]) ? 0 : 1;
+// the sum over a workgroup of each thread's n; red: one entry for each wave
+__device__ __forceinline__ int block_count(int n, int* red) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
@@ -349,6 +347,13 @@ __device__ __forceinline__ int count_rows(const RowArgs& a, int begin, int end, 
   n = 0;
   for (int i = 0; i < (int)blockDim.x / 64; i++) n += red[i];
   return n;
+}
+// unmasked rows among [begin, end), by all threads of a workgroup
+__device__ __forceinline__ int count_rows(const RowArgs& a, int begin, int end, int* red) {
+  int n = 0;
+#pragma unroll 8
+  for (int r = begin + (int)threadIdx.x; r < end; r += blockDim.x) n += a.masked(a.label[r]) ? 0 : 1;
+  return block_count(n, red);
 }
 // ---- rows.  Both kernels below go over the rows r = first, first + step, ...; the threads of a row ("team") are t = 0 .. TPR - 1.  Vectors of a row are those that
 // begin at multiples of 16 bytes: vector v of thread t at element head + (v * TPR + t) * N.  What lies in front of the first and behind the last is one element each of the
@@ -379,13 +384,12 @@ struct LabelAt {
   }
 };
 
+// the weight of an unmasked row
 __device__ __forceinline__ double unit_weight(const RowArgs& a, const int* counts, int n_counts, int* red) {
+  if (n_counts == 0) return 1.0 / count_rows(a, 0, a.rows, red);
   int n = 0;
-  if (n_counts)
-    for (int i = 0; i < n_counts; i++) n += counts[i];
-  else
-    n = count_rows(a, 0, a.rows, red);
-  return 1.0 / n;
+  for (int i = threadIdx.x; i < n_counts; i += blockDim.x) n += counts[i];
+  return 1.0 / block_count(n, red);
 }
 
 // a row's other inputs
@@ -721,6 +725,9 @@ struct RowPlan {
 // Sixteen vectors a thread (of both rows together) and sixteen waves on a compute unit are what its registers hold.  Where nothing is written rows need not stay: they are
 // streamed, a workgroup each, more of them at once than run, so that none has much more of them than another (2048 rows of 32000 classes of which one in five is
 // masked take 26 us, over the workgroups that run at once 37).
+// Rows no more than compute units leave them idle, so such a row takes more waves: with a gradient eight from 1024 vectors on (256 rows of 32000 classes in bf16 13.9 us instead of
+// 15.4; below, 64 rows of 8000 take 9.1 with four and 9.4 with eight), without one sixteen from 2048 on (64 rows of 128000 classes 14.5 us instead of 22.4; one row of 16400,
+// 7.8 with four and 8.1 with sixteen).
 // Past the caches goes what is read once: statistics of 7148 rows of 100003 classes 198 us instead of 228, the whole preference loss 632 instead of 662.  What the last-level
 // cache holds (256 MB) until the gradient's pass or the next kernel reads it is left there: four short pairs of 32000 classes, 63 MB, would take 45 us instead of 40.  Loads and stores
 // of gradients that it cannot hold: exact divergence of 4096 rows of 50257 classes 265 us instead of 273, policy loss of 8192 of 128000 815 instead of 823.
@@ -729,8 +736,9 @@ inline RowPlan row_plan(int rows, int classes, size_t size, bool full, bool grad
   const int64_t vecs = ((int64_t)classes * (int64_t)size + 15) / 16, most = full ? 8 : 16;
   const double bytes = (double)rows * classes * size;
   if (vecs <= 64 * (full ? 4 : 8)) return {1, true, 4 * cus, false};
-  if (!grad) return {4, false, MAX_GRID, !again || bytes > CACHED};
-  const bool nt = bytes > CACHED;
+  const bool nt = bytes > CACHED, few = rows <= cus;
+  if (!grad) return {few && vecs > 2048 ? 16 : 4, false, MAX_GRID, !again || nt};
+  if (few && vecs > 1024 && vecs <= 512 * most) return {8, true, cus, nt};
   if (vecs <= 256 * most) return {4, true, 4 * cus, nt};
   if (vecs <= 512 * most) return {8, true, 2 * cus, nt};
   if (vecs <= 1024 * most) return {16, true, cus, nt};
@@ -757,7 +765,9 @@ void row_launch(const RowPlan& plan, int grid, hipStream_t s, const RowCall& c) 
     if (c.a.classes * sizeof(T) <= 64 * 16 * 2) ET_ROW(kept_kernel, 1, 2, false);
     else ET_ROW(kept_kernel, 1, 8 / F, false);
   } else if constexpr (!GRAD) {
-    if (plan.nt) ET_ROW(streamed_kernel, 4, 8 / F, true);
+    if (plan.waves == 16 && plan.nt) ET_ROW(streamed_kernel, 16, 8 / F, true);
+    else if (plan.waves == 16) ET_ROW(streamed_kernel, 16, 8 / F, false);
+    else if (plan.nt) ET_ROW(streamed_kernel, 4, 8 / F, true);
     else ET_ROW(streamed_kernel, 4, 8 / F, false);
   } else if (!plan.keep) {
     ET_ROW(streamed_kernel, 4, 8 / F, false);

@@ -227,3 +227,14 @@ def test_scaling_by_a_norm_from_elsewhere(norm, out, bf16):
     torch.cuda.synchronize()
     f = 0.375 if norm == 2.0 else 1.0
     assert all((np.abs(v.double().cpu().numpy() - f * h) <= (2.0 ** -8 if bf16 else 2.0 ** -24) * np.abs(h) * (f != 1)).all() for v, h in zip(c.outs, c.host))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("out", [None, 0, 1])
+def test_more_than_the_caches_hold(out, bf16):
+    """Past 128 MB, and past what a launch reads without keeping it, with tensors on both sides of each border."""
+    n = 2 if bf16 else 1
+    c = Case([30_000_001 * n, 7, 26_000_003 * n, 300, 4_000_000], bf16, out=out, gap=1)
+    max_norm = float(np.float32(0.5 * losses.grad_norm(c.host)[0]))
+    c.call().check_norm()
+    c.call(max_norm).check_clip(max_norm)

@@ -272,3 +272,73 @@ def test_two_calls_at_once():
 
 def test_offsets_beyond_32_bits():
     Case(3, 1000, True, stride=1_200_000_001, gstride=1_100_000_003, masked=0).call().check()
+
+
+@pytest.mark.parametrize("rows,C,bf16,kl,train", [(300, 20000, True, "sampled", True), (260, 16001, False, "none", True), (300, 70001, True, "sampled", True),
+                                                  (300, 20000, True, "sampled", False), (257, 9000, False, "full", False), (200, 40000, True, "full", False)])
+def test_more_rows_than_compute_units_and_fewer(rows, C, bf16, kl, train):
+    Case(rows, C, bf16, kl, seed=3, train=train, masked=0.1).call().check()
+
+
+@pytest.mark.parametrize("train", [True, False])
+@pytest.mark.parametrize("rows,C,bf16", [(8192, 7, True), (8193, 40, False), (20000, 7, False), (40001, 9, True)])
+def test_many_rows_of_one_weight(rows, C, bf16, train):
+    Case(rows, C, bf16, seed=4, train=train).call().check()
+
+
+@pytest.mark.parametrize("kl", ["sampled", "full"])
+@pytest.mark.parametrize("C,bf16", [(200, True), (3001, False), (40001, True)])
+def test_captured_with_many_rows_of_one_weight(C, bf16, kl):
+    """More rows than one workgroup counts, with labels that change between replays, so that the weight of a row does."""
+    import torch
+    rows = 8200 if C < 1000 else 300
+    c = Case(rows, C, bf16, kl, seed=5).call()
+    graph, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=s):
+        c.go(torch.cuda.current_stream().cuda_stream)
+    kept = c.d["label"].clone()
+    for k in range(3):
+        c.d["label"].copy_(kept)
+        c.d["label"][:rows // 3 * k] = -1
+        c.call(ws=c.ws)
+        want = [v.clone() for v in (c.grad.flat, c.logp)]
+        loss, stats = c.loss.clone(), c.stats.clone()
+        c.grad.flat.fill_(-3.0), c.ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(want[0], c.grad.flat), k
+        assert torch.isfinite(loss).all() and torch.isfinite(stats).all()
+
+
+@pytest.mark.parametrize("kl", ["sampled", "full"])
+@pytest.mark.parametrize("rows,C,bf16,train", [(2100, 50257, True, True), (900, 128000, True, True), (4200, 24001, True, True), (1100, 50257, False, True),
+                                               (2100, 50257, True, False)])
+def test_more_logits_than_the_caches_hold(rows, C, bf16, train, kl):
+    """The same bits as from parts of the rows, small enough to stay in the caches."""
+    import torch
+    from paper_2312_14227_amd import binding as et
+    torch.manual_seed(rows)
+    ty, dtype = (et.ET_BF16, torch.bfloat16) if bf16 else (et.ET_F32, torch.float32)
+    x = torch.randn(rows, C, device="cuda", dtype=dtype) * 2
+    y = x + torch.randn(1, C, device="cuda", dtype=dtype) / 4
+    label = torch.randint(0, C, (rows,), device="cuda", dtype=torch.int32)
+    label[::7] = -1
+    old, adv, weight = -8 + torch.randn(rows, device="cuda"), torch.randn(rows, device="cuda"), torch.rand(rows, device="cuda")
+
+    def run(at, n, grad, logp):
+        ws, loss = torch.full((et.et_policy_loss_ws_bytes(n),), 0xFF, dtype=torch.uint8, device="cuda"), torch.zeros(1, device="cuda")
+        kw = dict(ref_logits=y[at:].data_ptr(), ref_stride=C) if kl == "full" else dict(ref_logp=old[at:].data_ptr())
+        p = et.make_policy(old[at:].data_ptr(), adv[at:].data_ptr(), weight=weight[at:].data_ptr(), clip_low=LOW, clip_high=HIGH, kl_coef=KL,
+                           logp=logp[at:].data_ptr(), **kw)
+        et.et_policy_loss(n, C, x[at:].data_ptr(), ty, C, label[at:].data_ptr(), p, grad[at:].data_ptr() if train else 0, ty, C, ws.data_ptr(), ws.numel(),
+                          torch.cuda.current_stream().cuda_stream, loss.data_ptr())
+        torch.cuda.synchronize()
+        return loss.item()
+
+    outs = [(torch.full_like(x, 7.0), torch.full((rows,), 7.0, device="cuda")) for _ in range(2)]
+    whole = run(0, rows, *outs[0])
+    step = (rows + 2) // 3
+    parts = [run(at, min(step, rows - at), *outs[1]) for at in range(0, rows, step)]
+    assert torch.equal(outs[0][1], outs[1][1]) and torch.equal(outs[0][0], outs[1][0])
+    assert abs(whole - sum(parts)) <= 1e-5 * sum(abs(v) for v in parts) + 1e-4

@@ -222,3 +222,103 @@ def test_the_same_bits_on_another_stream():
 
 def test_offsets_beyond_32_bits():
     Case([1, 2], 1000, True, pad=1_200_000_001, gpad=1_100_000_003, masked=0).call().check()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("C", [1, 2, 7, 40, 200, 511, 777, 1000, 1024, 1025, 2047, 2048, 2049])
+def test_pairs_of_single_rows(C, bf16):
+    Case([1] * 14, C, bf16, offsets=False, eps=0.1).call().check()
+
+
+@pytest.mark.parametrize("bf16,gbf16", [(False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("C,skip,gskip,pad,gpad", [(200, 1, 0, 0, 0), (301, 3, 5, 1, 0), (1000, 0, 1, 47, 3), (13, 2, 2, 6, 6)])
+def test_strides_of_single_rows(C, skip, gskip, pad, gpad, bf16, gbf16):
+    Case([1] * 10, C, bf16, gbf16, offsets=False, skip=skip, gskip=gskip, pad=pad, gpad=gpad).call().check()
+
+
+@pytest.mark.parametrize("train", [True, False])
+@pytest.mark.parametrize("C", [200, 999])
+def test_single_rows_in_place_and_without_a_gradient(C, train):
+    Case([1] * 10, C, True, offsets=False, in_place=train, train=train, pad=5, skip=3).call().check()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("C", [40, 200, 1000])
+def test_masked_logits_and_single_rows(C, bf16):
+    lowest = -3.3895313892515355e38 if bf16 else -3.4028234663852886e38
+
+    def edit(c):
+        rng = np.random.default_rng(4)
+        c.label[:] = rng.integers(0, C, c.rows)
+        own = np.arange(C) == c.label[:, None]
+        off = (rng.random(c.x.shape) < 0.5) & ~own
+        c.x[0][off[0]], c.x[1][off[1]] = -np.inf, lowest
+        c.x[2], c.x[3] = -np.inf, lowest
+        c.x[4] = np.where(own[4], 0, -np.inf)
+        c.x[5][own[5]] = 30
+        c.label[[6, 7, 8, 11]] = [-1, C, -2 ** 31, 2 ** 31 - 1]
+        c.x[[6, 7]], c.x[[8, 11]] = np.nan, np.inf
+        c.ref[:] = np.float32(losses.preference_loss(c.x, c.label, c.offsets, 1.0)["logp"] - 1)
+
+    Case([1] * 12, C, bf16, offsets=False, edit=edit).call().check()
+
+
+@pytest.mark.parametrize("offsets", [False, True])
+def test_not_a_number_stays_in_its_pair(offsets):
+    def edit(c):
+        c.label[:] = 5
+        c.x[2, 7] = np.nan
+
+    c = Case([1] * 6, 300, True, offsets=offsets, edit=edit, masked=0, ref=False).call()
+    g = c.grad.host()
+    assert np.isnan(g[2:4]).all() and np.isfinite(g[[0, 1, 4, 5]]).all() and np.isnan(c.loss.item())
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_single_rows_captured_and_replayed(bf16):
+    import torch
+    c = Case([1] * 40, 200, bf16, offsets=False).call()
+    other = Case([1] * 40, 200, bf16, offsets=False, seed=9).call()
+    graph, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=s):
+        c.go(torch.cuda.current_stream().cuda_stream)
+    want = [[t.clone() for t in v.outputs()] for v in (c, other)]
+    inputs = [c.logits.flat, c.d[0], c.d[2]]
+    values = [[t.clone() for t in inputs], [other.logits.flat, other.d[0], other.d[2]]]
+    for k in range(4):
+        for t, v in zip(inputs, values[k % 2]):
+            t.copy_(v)
+        for t in c.outputs():
+            t.fill_(-3.0)
+        c.ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want[k % 2], c.outputs())), k
+
+
+@pytest.mark.parametrize("rows,C,bf16", [(4096, 24576, True), (2048, 50257, False)])
+def test_more_logits_than_the_caches_hold(rows, C, bf16):
+    """Sums of the same bits as from a half of the pairs, which stays in the caches, and gradients of half its size (a power of two: exactly)."""
+    import torch
+    from paper_2312_14227_amd import binding as et
+    torch.manual_seed(rows)
+    ty, dtype = (et.ET_BF16, torch.bfloat16) if bf16 else (et.ET_F32, torch.float32)
+    x = torch.randn(rows, C, device="cuda", dtype=dtype)
+    label = torch.randint(0, C, (rows,), device="cuda", dtype=torch.int32)
+    label[::5] = -1
+    grads = [torch.full_like(x, 7.0) for _ in range(2)]
+    logp = [torch.zeros(8, device="cuda") for _ in range(2)]
+    offsets = torch.arange(9, device="cuda", dtype=torch.int32) * (rows // 8)
+
+    def run(k, at, n, pairs):
+        ws, loss = torch.full((et.et_preference_loss_ws_bytes(n, pairs),), 0xFF, dtype=torch.uint8, device="cuda"), torch.zeros(1, device="cuda")
+        p = et.make_preference(offsets.data_ptr(), 0, 0.001, 0.0, logp[k][at * 8 // rows:].data_ptr(), 0)
+        et.et_preference_loss(n, pairs, C, x[at:].data_ptr(), ty, C, label[at:].data_ptr(), p, grads[k][at:].data_ptr(), ty, C, ws.data_ptr(), ws.numel(),
+                              torch.cuda.current_stream().cuda_stream, loss.data_ptr())
+        torch.cuda.synchronize()
+
+    run(0, 0, rows, 4)
+    for at in (0, rows // 2):
+        run(1, at, rows // 2, 2)
+    assert torch.equal(logp[0], logp[1]) and torch.equal(grads[0] * 2, grads[1])
