@@ -284,7 +284,9 @@ int et_train_step(et_ctx* ctx, const void* x_dev, const int32_t* y_dev, const ui
  * any state; a call leaves nothing in it that a later one reads.  Calls (and replays of captured ones) that share a workspace must not overlap.
  * Sums run in a fixed order: a call on the same inputs gives the same bits.  ET_ENOMEM: the workspace is too small.
  *
- * Logits: row r of `classes` (at most 2^28) values starts at logits_dev + r * row_stride (in elements, row_stride >= classes), of type `dtype` (ET_F32 |
+ * Outputs must not overlap anything else that a call reads or writes, but where it is said that they may.
+ *
+ * Logits: row r (of at most 2^30) of `classes` (at most 2^28) values starts at logits_dev + r * row_stride (in elements, row_stride >= classes), of type `dtype` (ET_F32 |
  * ET_BF16).  The gradient has the same shape, a stride and a type of its own; grad_dev == NULL: no gradient is computed.  It may be logits_dev itself
  * (same stride and type), and must not overlap the logits otherwise (ET_EINVAL).  Pointers need their element's alignment only.  Elements between the rows are
  * neither read nor written.  label_dev[r] is the row's class (the action taken, the token produced); one outside [0, classes) masks the
@@ -324,7 +326,7 @@ int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_
  * one of pair p, 2p + 1 the other.  With L[i] the sum of its unmasked rows' log probabilities of their labels (0 of an empty sequence):
  *   z = beta * ((L[2p] - ref[2p]) - (L[2p+1] - ref[2p+1]))
  *   loss = mean over pairs of -(1 - label_smoothing) log sigmoid(z) - label_smoothing log sigmoid(-z)
- * Rows in front of the first sequence and behind the last are neither read nor written.  Offsets that descend or leave [0, rows]
+ * At most 2^23 pairs.  Rows in front of the first sequence and behind the last are neither read nor written.  Offsets that descend or leave [0, rows]
  * are cut to where they do not. */
 typedef struct {
   const int32_t* offsets_dev;   /* [2 pairs + 1], ascending; NULL: every row is a sequence (rows = 2 pairs) */
@@ -341,14 +343,14 @@ int et_preference_loss(int32_t rows, int32_t pairs, int32_t classes, const void*
 
 /* Euclidean norm of n gradients as one vector, and (tensor_norm_dev [n], or NULL) of each.  grad_dev and numel are host arrays; tensors are
  * contiguous, of type `dtype`, aligned to their element; numel[i] = 0 is allowed (the pointer is not used then), n = 0 too (norm 0).
- * Squares are added in float64: no overflow or underflow inside. */
+ * n is at most 2^21.  Squares are added in float64: no overflow or underflow inside. */
 size_t et_grad_norm_ws_bytes(int32_t n, const uint64_t* numel);
 int et_grad_norm(int32_t n, const void* const* grad_dev, const uint64_t* numel, int32_t dtype, void* workspace_dev, size_t workspace_bytes,
                  void* hip_stream, float* norm_dev, float* tensor_norm_dev);
 
 /* The same, and clipping: out[i] = grad[i] * c, c = max_norm / norm if norm > max_norm, else 1, with the norm and c each rounded to float32.  A norm that is not
  * finite leaves the values as they are: the caller sees it in norm_dev.  out_dev == NULL or out_dev[i] == grad_dev[i]: in place (nothing is written where c = 1);
- * otherwise out[i] must not overlap any gradient.  In place a tensor may be listed once only.  max_norm >= 0.  Workspace: et_grad_norm_ws_bytes. */
+ * otherwise out[i] must not overlap any gradient.  No two outputs may overlap: in place a tensor is listed once only (else ET_EINVAL).  max_norm >= 0.  Workspace: et_grad_norm_ws_bytes. */
 int et_grad_clip(int32_t n, const void* const* grad_dev, void* const* out_dev, const uint64_t* numel, int32_t dtype, float max_norm,
                  void* workspace_dev, size_t workspace_bytes, void* hip_stream, float* norm_dev, float* tensor_norm_dev);
 

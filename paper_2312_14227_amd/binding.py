@@ -381,19 +381,27 @@ def et_grad_norm_ws_bytes(numel):
     return _lib.et_grad_norm_ws_bytes(len(numel), sizes(numel))
 
 
+def _same_length(where, numel, *lists):
+    if any(len(v) != len(numel) for v in lists if v is not None):
+        raise EtError(ET_EINVAL, where)
+
+
 def et_grad_norm(grad, numel, dtype, ws, ws_bytes, stream, norm, tensor_norm=0):
     """grad, numel: lists, or what pointers() and sizes() made of them."""
+    _same_length("et_grad_norm", numel, grad)
     _check(_lib.et_grad_norm(len(numel), _ptr_array(grad), sizes(numel), dtype, ws, ws_bytes, stream, norm, tensor_norm), "et_grad_norm")
 
 
 def et_grad_clip(grad, out, numel, dtype, max_norm, ws, ws_bytes, stream, norm, tensor_norm=0):
     """out: like grad, or None to clip in place."""
+    _same_length("et_grad_clip", numel, grad, out)
     _check(_lib.et_grad_clip(len(numel), _ptr_array(grad), _ptr_array(out) if out is not None else None, sizes(numel), dtype, max_norm, ws, ws_bytes, stream,
                              norm, tensor_norm), "et_grad_clip")
 
 
 def et_grad_scale(grad, out, numel, dtype, norm, max_norm, stream):
     """norm: the device address of one; out as in et_grad_clip."""
+    _same_length("et_grad_scale", numel, grad, out)
     _check(_lib.et_grad_scale(len(numel), _ptr_array(grad), _ptr_array(out) if out is not None else None, sizes(numel), dtype, norm, max_norm, stream),
            "et_grad_scale")
 

@@ -4,7 +4,10 @@
 // units do in the time that memory takes), one launch adds the chunks: a workgroup all of them, and one for each tensor its own.  Clipping goes over the chunks once more,
 // from the last to the first, so that what the norm has read last is found in the caches.  The table of tensors travels as kernel arguments: nothing is
 // copied from the host.  No atomics: the order of every sum is fixed.
+#include <algorithm>
 #include <cmath>
+#include <new>
+#include <vector>
 
 #include "context.h"
 #include "op_args.h"
@@ -221,16 +224,53 @@ bool make_plan(int32_t n, const uint64_t* numel, Plan* p) {
 }
 size_t ws_bytes(int32_t n, const Plan& p) { return 64 + sizeof(double) * (size_t)p.chunks + sizeof(uint32_t) * (size_t)n; }
 
-int check_tensors(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, int32_t dtype, const float* norm) {
-  if (n < 0 || (n > 0 && (!grad || !numel)) || !type_ok(dtype) || !norm || !aligned(norm, 4)) return ET_EINVAL;
+// Whether what is written (out, or in place: grad) meets anything that another tensor reads or writes.  Tensors of an arena, in its order, are seen to be apart in one pass.
+bool apart(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, size_t size) {
+  struct Piece {
+    uintptr_t begin, end;
+    bool written;
+  };
+  uintptr_t last = 0;
+  bool ascending = true;
+  for (int32_t i = 0; i < n && ascending; i++) {
+    if (numel[i] == 0) continue;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(grad[i]);
+    ascending = (!out || out[i] == grad[i]) && at >= last;
+    last = at + numel[i] * size;
+  }
+  if (ascending) return true;
+  std::vector<Piece> all;
+  all.reserve(2 * (size_t)n);
+  for (int32_t i = 0; i < n; i++) {
+    if (numel[i] == 0) continue;
+    const uintptr_t g = reinterpret_cast<uintptr_t>(grad[i]), o = out ? reinterpret_cast<uintptr_t>(out[i]) : g;
+    all.push_back({o, o + numel[i] * size, true});
+    if (o != g) all.push_back({g, g + numel[i] * size, false});
+  }
+  std::sort(all.begin(), all.end(), [](const Piece& a, const Piece& b) { return a.begin < b.begin; });
+  uintptr_t read = 0, written = 0;   // where what begins at or in front of a piece ends
+  for (const Piece& p : all) {
+    if (p.begin < written || (p.written && p.begin < read)) return false;
+    uintptr_t& end = p.written ? written : read;
+    end = std::max(end, p.end);
+  }
+  return true;
+}
+
+// writes: whether tensors are scaled (in place, if out is null)
+int check_tensors(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, int32_t dtype, const float* norm, bool writes) {
+  if (n < 0 || n > 1 << 21 || (n > 0 && (!grad || !numel)) || !type_ok(dtype) || !norm || !aligned(norm, 4)) return ET_EINVAL;
   const size_t size = type_size(dtype);
   for (int32_t i = 0; i < n; i++) {
     if (numel[i] == 0) continue;
     const void* o = out ? out[i] : grad[i];
     if (!grad[i] || !o || !aligned(grad[i], size) || !aligned(o, size) || numel[i] > (1ull << 48)) return ET_EINVAL;
-    if (o != grad[i] && Span(grad[i], 1, (int64_t)numel[i], 0, size).meets(Span(o, 1, (int64_t)numel[i], 0, size))) return ET_EINVAL;
   }
-  return ET_OK;
+  try {
+    return !writes || apart(n, grad, out, numel, size) ? ET_OK : ET_EINVAL;
+  } catch (const std::bad_alloc&) {
+    return ET_ENOMEM;
+  }
 }
 
 // fills the table of the launch that begins with tensor `first`; next: its first chunk, and what follows its last
@@ -281,7 +321,7 @@ void scale_launch(int32_t n, const void* const* grad, void* const* out, const ui
 // max_norm < 0: the norm only
 int norm_and_clip(int32_t n, const void* const* grad, void* const* out, const uint64_t* numel, int32_t dtype, float max_norm, void* ws, size_t bytes,
                   void* hip_stream, float* norm, float* tensor_norm) {
-  const int rc = check_tensors(n, grad, out, numel, dtype, norm);
+  const int rc = check_tensors(n, grad, out, numel, dtype, norm, max_norm >= 0);
   if (rc != ET_OK) return rc;
   if (!ws || !aligned(ws, 16) || !aligned(tensor_norm, 4)) return ET_EINVAL;
   Plan p;
@@ -301,7 +341,7 @@ extern "C" {
 
 size_t et_grad_norm_ws_bytes(int32_t n, const uint64_t* numel) {
   Plan p;
-  return n < 0 || (n > 0 && !numel) || !make_plan(n, numel, &p) ? 0 : ws_bytes(n, p);
+  return n < 0 || n > 1 << 21 || (n > 0 && !numel) || !make_plan(n, numel, &p) ? 0 : ws_bytes(n, p);
 }
 
 int et_grad_norm(int32_t n, const void* const* grad_dev, const uint64_t* numel, int32_t dtype, void* workspace_dev, size_t workspace_bytes,
@@ -318,7 +358,7 @@ int et_grad_clip(int32_t n, const void* const* grad_dev, void* const* out_dev, c
 int et_grad_scale(int32_t n, const void* const* grad_dev, void* const* out_dev, const uint64_t* numel, int32_t dtype, const float* norm_dev, float max_norm,
                   void* hip_stream) {
   if (!(max_norm >= 0)) return ET_EINVAL;
-  const int rc = check_tensors(n, grad_dev, out_dev, numel, dtype, norm_dev);
+  const int rc = check_tensors(n, grad_dev, out_dev, numel, dtype, norm_dev, true);
   if (rc != ET_OK) return rc;
   Plan p;
   if (!make_plan(n, numel, &p)) return ET_EINVAL;

@@ -252,12 +252,16 @@ using namespace et_op;
 constexpr int MAX_COUNTS = 256;
 constexpr size_t POLICY_WS = sizeof(int) * MAX_COUNTS + sizeof(double) * et::rows::COLUMNS * 4 * et::rows::MAX_GRID;
 
+constexpr int MOST_PAIRS = 1 << 23;   // (a workgroup each: what a launch can have)
 size_t preference_ws(int64_t rows, int64_t pairs) { return (size_t)(rows * 24 + pairs * 24 + 256); }
+
+// whether vectors of n floats, either may be missing, have a byte in common
+bool meet(const float* a, const float* b, int64_t n) { return a && b && Span(a, 1, n, 0, 4).meets(Span(b, 1, n, 0, 4)); }
 
 // the arguments that both losses have in common
 int check_rows(int32_t rows, int32_t classes, const void* logits, int32_t dtype, int64_t stride, const int32_t* label, const void* grad,
                int32_t grad_dtype, int64_t grad_stride, const void* ws, const float* loss) {
-  if (rows < 1 || classes < 1 || classes > 1 << 28 || !logits || !label || !ws || !loss || !type_ok(dtype) || (grad && !type_ok(grad_dtype))) return ET_EINVAL;
+  if (rows < 1 || rows > 1 << 30 || classes < 1 || classes > 1 << 28 || !logits || !label || !ws || !loss || !type_ok(dtype) || (grad && !type_ok(grad_dtype))) return ET_EINVAL;
   const int64_t most = (INT64_MAX >> 4) / rows;   // (offsets in bytes stay below 2^62)
   if (stride < classes || stride > most || (grad && (grad_stride < classes || grad_stride > most))) return ET_EINVAL;
   if (!aligned(logits, type_size(dtype)) || !aligned(label, 4) || !aligned(loss, 4) || !aligned(ws, 16)) return ET_EINVAL;
@@ -278,6 +282,8 @@ int et_op::policy_loss(int32_t rows, int32_t classes, const void* logits_dev, in
   if (!p || !p->old_logp_dev || !p->advantage_dev || (p->ref_logp_dev && p->ref_logits_dev)) return ET_EINVAL;
   for (const float* v : {p->old_logp_dev, p->advantage_dev, p->ref_logp_dev, p->weight_dev, (const float*)p->logp_dev, (const float*)p->stats_dev})
     if (!aligned(v, 4)) return ET_EINVAL;
+  for (const float* v : {p->old_logp_dev, p->advantage_dev, p->ref_logp_dev, p->weight_dev})
+    if (meet(v, p->logp_dev, rows)) return ET_EINVAL;
   if (!(p->clip_low >= 0 && p->clip_low <= 1 && p->clip_high >= 0 && std::isfinite(p->clip_high) && std::isfinite(p->kl_coef))) return ET_EINVAL;
   if (p->ref_logits_dev) {
     if (p->ref_stride < classes || p->ref_stride > (INT64_MAX >> 4) / rows || !aligned(p->ref_logits_dev, type_size(dtype))) return ET_EINVAL;
@@ -318,8 +324,9 @@ int et_op::preference_loss(int32_t rows, int32_t pairs, int32_t classes, const v
                            float* loss_dev, bool check_only, int* launches) {
   const int rc = check_rows(rows, classes, logits_dev, dtype, row_stride, label_dev, grad_dev, grad_dtype, grad_stride, workspace_dev, loss_dev);
   if (rc != ET_OK) return rc;
-  if (!p || pairs < 1 || pairs > (INT32_MAX - 1) / 2 || (!p->offsets_dev && rows != 2 * pairs)) return ET_EINVAL;
+  if (!p || pairs < 1 || pairs > MOST_PAIRS || (!p->offsets_dev && rows != 2 * pairs)) return ET_EINVAL;
   if (!aligned(p->offsets_dev, 4) || !aligned(p->ref_logp_dev, 4) || !aligned(p->logp_dev, 4) || !aligned(p->stats_dev, 4)) return ET_EINVAL;
+  if (meet(p->ref_logp_dev, p->logp_dev, 2 * (int64_t)pairs)) return ET_EINVAL;
   if (!(p->beta > 0 && std::isfinite(p->beta) && p->label_smoothing >= 0 && p->label_smoothing <= 1)) return ET_EINVAL;
   if (workspace_bytes < preference_ws(rows, pairs)) return ET_ENOMEM;
   if (check_only) return ET_OK;
@@ -372,8 +379,8 @@ int et_op::preference_loss(int32_t rows, int32_t pairs, int32_t classes, const v
 
 extern "C" {
 
-size_t et_policy_loss_ws_bytes(int32_t rows) { return rows < 1 ? 0 : POLICY_WS; }
-size_t et_preference_loss_ws_bytes(int32_t rows, int32_t pairs) { return rows < 1 || pairs < 1 ? 0 : preference_ws(rows, pairs); }
+size_t et_policy_loss_ws_bytes(int32_t rows) { return rows < 1 || rows > 1 << 30 ? 0 : POLICY_WS; }
+size_t et_preference_loss_ws_bytes(int32_t rows, int32_t pairs) { return rows < 1 || rows > 1 << 30 || pairs < 1 || pairs > MOST_PAIRS ? 0 : preference_ws(rows, pairs); }
 
 int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_t dtype, int64_t row_stride, const int32_t* label_dev,
                    const et_policy* policy, void* grad_dev, int32_t grad_dtype, int64_t grad_stride, void* workspace_dev, size_t workspace_bytes,

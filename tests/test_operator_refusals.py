@@ -80,3 +80,48 @@ def test_grad_scale_refuses(kw):
     with pytest.raises(et.EtError) as e:
         et.et_grad_scale(a["grad"], a["out"], a["numel"], a["dtype"], a["norm"], a["max_norm"], 0)
     assert e.value.status == et.ET_EINVAL
+
+
+OVERLAPS = [(["a", "a"], None), (["a", "a+4"], None), (["b", "a", "a+28"], None), (["a", "b"], ["c", "c"]), (["a", "b"], ["c", "c+4"]), (["a", "b"], ["b", "c"]), (["a", "b"], ["c", "a"]),
+            (["a", "b"], ["b", "a"]), (["a", "b"], ["a", "a+16"]), (["a", "b"], ["c", "a-4"]), (["c", "b", "a"], ["c", "b", "b+12"]), (["a", "a"], ["a", "c"])]
+
+
+@pytest.mark.parametrize("grad,out", OVERLAPS)
+def test_outputs_that_meet_another_tensor(grad, out):
+    at = lambda names: None if names is None else [eval(s, {"a": A, "b": A + 4096, "c": A + 8192}) for s in names]  # noqa: E731
+    n = [8] * len(grad)
+    for call in (lambda: et.et_grad_clip(at(grad), at(out), n, et.ET_F32, 1.0, A, 1 << 20, 0, A), lambda: et.et_grad_scale(at(grad), at(out), n, et.ET_F32, A, 1.0, 0)):
+        with pytest.raises(et.EtError) as e:
+            call()
+        assert e.value.status == et.ET_EINVAL
+
+
+def test_lists_of_other_lengths():
+    for grad, out in (([A], None), ([A, 2 * A, 3 * A], None), ([A, 2 * A], [A])):
+        with pytest.raises(et.EtError):
+            et.et_grad_clip(grad, out, [8, 8], et.ET_F32, 1.0, A, 1 << 20, 0, A)
+        with pytest.raises(et.EtError):
+            et.et_grad_scale(grad, out, [8, 8], et.ET_F32, A, 1.0, 0)
+    with pytest.raises(et.EtError):
+        et.et_grad_norm([A], [8, 8], et.ET_F32, A, 1 << 20, 0, A)
+
+
+def test_outputs_on_the_inputs():
+    B = 1 << 30
+    for kw in (dict(logp=A), dict(old=B, logp=B + 12), dict(ref_logp=B, logp=B - 12), dict(weight=B, logp=B)):
+        with pytest.raises(et.EtError) as e:
+            _policy(**kw)
+        assert e.value.status == et.ET_EINVAL
+    for kw in (dict(ref_logp=B, logp=B), dict(ref_logp=B, logp=B + 12)):
+        with pytest.raises(et.EtError) as e:
+            _preference(**kw)
+        assert e.value.status == et.ET_EINVAL
+
+
+def test_more_than_any_call_takes():
+    for call, kw in ((_policy, dict(rows=(1 << 30) + 1)), (_preference, dict(rows=(1 << 30) + 1)), (_preference, dict(pairs=(1 << 23) + 1, rows=1 << 25))):
+        with pytest.raises(et.EtError) as e:
+            call(grad=0, ws_bytes=1 << 50, **kw)
+        assert e.value.status == et.ET_EINVAL
+    assert et.et_policy_loss_ws_bytes((1 << 30) + 1) == 0 and et.et_preference_loss_ws_bytes(1 << 25, (1 << 23) + 1) == 0
+    assert et.et_policy_loss_ws_bytes(1 << 30) > 0 and et.et_preference_loss_ws_bytes(1 << 30, 1 << 23) > 0
