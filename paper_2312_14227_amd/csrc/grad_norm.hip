@@ -212,7 +212,7 @@ uint32_t cached_from(const Plan& p, size_t size) {
 }
 
 // False: a size that no memory holds.  Chunks of 64 KB where there are enough of them, so that a workgroup's beginning and end are a small part of it;
-// smaller ones spread few elements over the chip (200 000 of them: 49 workgroups of 4096, 6.0 us, or 13 of 16384, 7.5); larger ones keep the sums of chunks few.
+// smaller ones spread few elements over the chip (200 000 float32: 49 workgroups of 4096, 5.1 us, or 13 of 16384, 5.6); larger ones keep the sums of chunks few.
 bool make_plan(int32_t n, const uint64_t* numel, Plan* p) {
   for (int32_t i = 0; i < n; i++) {
     if (numel[i] > (1ull << 48) || (p->total += numel[i]) > (1ull << 48)) return false;

@@ -5,7 +5,8 @@
 // p[a] is close to 1.
 //
 // What bounds them: memory, with the vector units close behind.  An element costs a row's statistics some 8 issue slots, four of them the exponential, and the
-// gradient 8 more; a row of 128000 bf16 classes takes a compute unit 18 us of those and 24 us of its share of the memory.
+// gradient 8 more: by count, a row of 128000 bf16 classes takes a compute unit 18 us of those and 24 us of its share of the memory.  Policy loss with gradient of 8192 such rows:
+// 813 us, 5.2 TB/s; its value alone of 2048 rows of 32000, one in five masked: 26.8 us, 3.9 TB/s; exact divergence of 4096 rows of 50257, one in ten masked: 264 us, 4.4 TB/s.
 #pragma once
 #include <cmath>
 #include <type_traits>
@@ -724,19 +725,21 @@ struct RowPlan {
 };
 // Sixteen vectors a thread (of both rows together) and sixteen waves on a compute unit are what its registers hold.  Where nothing is written rows need not stay: they are
 // streamed, a workgroup each, more of them at once than run, so that none has much more of them than another (2048 rows of 32000 classes of which one in five is
-// masked take 26 us, over the workgroups that run at once 37).
-// Rows no more than compute units leave them idle, so such a row takes more waves: with a gradient eight from 1024 vectors on (256 rows of 32000 classes in bf16 13.9 us instead of
-// 15.4; below, 64 rows of 8000 take 9.1 with four and 9.4 with eight), without one sixteen from 2048 on (64 rows of 128000 classes 14.5 us instead of 22.4; one row of 16400,
-// 7.8 with four and 8.1 with sixteen).
-// Past the caches goes what is read once: statistics of 7148 rows of 100003 classes 198 us instead of 228, the whole preference loss 632 instead of 662.  What the last-level
-// cache holds (256 MB) until the gradient's pass or the next kernel reads it is left there: four short pairs of 32000 classes, 63 MB, would take 45 us instead of 40.  Loads and stores
-// of gradients that it cannot hold: exact divergence of 4096 rows of 50257 classes 265 us instead of 273, policy loss of 8192 of 128000 815 instead of 823.
+// masked take 26.8 us, over the workgroups that run at once 28.3).
+// A row that a wave's registers hold takes one (16384 rows of 4000 bf16 classes 59 us, with four waves 88).
+// Rows no more than compute units leave them idle, so such a row takes more waves: four from a half of a wave's registers on (64 rows of 4000 8.5 us instead of 9.9); with a
+// gradient eight from 1024 vectors on (256 rows of 32000 13.9 us instead of 15.4; below, 64 rows of 8000 take 9.1 with four and 9.4 with eight); without one sixteen from 2048 on
+// (64 rows of 128000 14.5 us instead of 22.4; one row of 16400 takes 7.8 with four and 8.1 with sixteen).
+// Past the caches goes what is read once: preference loss of 7148 rows of 100003 classes 626 us instead of 656, values of 2048 rows of 32000 26.8 instead of 27.8.  What the last-level
+// cache holds (256 MB) until the gradient's pass or the next kernel reads it is left there: four short pairs of 32000 classes, 63 MB, would take 41.1 us instead of 35.8.  Loads and stores
+// of gradients that it cannot hold: exact divergence of 4096 rows of 50257 classes 264 us instead of 273, policy loss of 8192 of 128000 813 instead of 824.
 constexpr double CACHED = 192e6;
 inline RowPlan row_plan(int rows, int classes, size_t size, bool full, bool grad, bool again, int cus) {
-  const int64_t vecs = ((int64_t)classes * (int64_t)size + 15) / 16, most = full ? 8 : 16;
+  const int64_t vecs = ((int64_t)classes * (int64_t)size + 15) / 16, most = full ? 8 : 16, alone = 64 * (full ? 4 : 8);
   const double bytes = (double)rows * classes * size;
-  if (vecs <= 64 * (full ? 4 : 8)) return {1, true, 4 * cus, false};
-  const bool nt = bytes > CACHED, few = rows <= cus;
+  const bool few = rows <= cus;
+  if (vecs <= (few ? alone / 2 : alone)) return {1, true, 4 * cus, false};
+  const bool nt = bytes > CACHED;
   if (!grad) return {few && vecs > 2048 ? 16 : 4, false, MAX_GRID, !again || nt};
   if (few && vecs > 1024 && vecs <= 512 * most) return {8, true, cus, nt};
   if (vecs <= 256 * most) return {4, true, 4 * cus, nt};
@@ -762,6 +765,7 @@ void row_launch(const RowPlan& plan, int grid, hipStream_t s, const RowCall& c) 
   hipLaunchKernelGGL((KERNEL<T, G, W, NV, MODE, GRAD, NT>), dim3(grid), dim3(W == 1 ? 256 : 64 * W), 0, s, c.a, c.p, c.seq, c.o, c.counts, c.n_counts, c.parts)
   constexpr bool SAME = std::is_same<T, G>::value;   // (a gradient of another type than the logits is rare: not both kinds of kernels)
   if (plan.waves == 1) {
+    // (16384 rows of 200 bf16 classes 26.9 us, as the first part of eight vectors 28.5)
     if (c.a.classes * sizeof(T) <= 64 * 16 * 2) ET_ROW(kept_kernel, 1, 2, false);
     else ET_ROW(kept_kernel, 1, 8 / F, false);
   } else if constexpr (!GRAD) {

@@ -342,3 +342,24 @@ def test_more_logits_than_the_caches_hold(rows, C, bf16, train, kl):
     parts = [run(at, min(step, rows - at), *outs[1]) for at in range(0, rows, step)]
     assert torch.equal(outs[0][1], outs[1][1]) and torch.equal(outs[0][0], outs[1][0])
     assert abs(whole - sum(parts)) <= 1e-5 * sum(abs(v) for v in parts) + 1e-4
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("C", [200, 6000, 140001])
+def test_a_class_that_the_reference_gives_probability_zero(C, bf16):
+    """1e30 stands for the infinite difference: the divergence is p of that class times that, and the other rows' stay as they are."""
+    def edit(c):
+        c.label[:] = 3
+        c.x[1, 9], c.y[1, 9] = c.x[1].max(), -np.inf
+        c.x[2, 9], c.y[2, 9] = -np.inf, -np.inf
+
+    c = Case(4, C, bf16, "full", edit=edit, masked=0).call()
+    p = np.exp(losses.log_softmax(c.x[1]))
+    kl = c.stats[1].item()
+    assert abs(kl - p[9] * 1e30 / 4) <= 1e-4 * p[9] * 1e30 / 4
+    g = c.grad.host()
+    assert np.isfinite(g).all() and abs(g[1, 9] - KL / 4 * p[9] * (1 - p[9]) * 1e30) <= (1e-4 + half_step(bf16)) * KL / 4 * p[9] * 1e30
+    kept, c.y[1, 9] = c.y[1, 9], c.x[1, 9]
+    w = c.want()["grad"]
+    c.y[1, 9] = kept
+    assert np.abs(g[[0, 2, 3]] - w[[0, 2, 3]]).max() <= 2 * half_step(bf16) * np.abs(w).max() + 1e-5 * np.abs(w).max()
