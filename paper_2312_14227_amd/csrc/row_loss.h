@@ -349,11 +349,17 @@ __device__ __forceinline__ int block_count(int n, int* red) {
   for (int i = 0; i < (int)blockDim.x / 64; i++) n += red[i];
   return n;
 }
-// unmasked rows among [begin, end), by all threads of a workgroup
+// unmasked rows among [begin, end), by all threads of a workgroup: their labels come sixteen a thread at once
 __device__ __forceinline__ int count_rows(const RowArgs& a, int begin, int end, int* red) {
+  constexpr int AT_ONCE = 16;
   int n = 0;
-#pragma unroll 8
-  for (int r = begin + (int)threadIdx.x; r < end; r += blockDim.x) n += a.masked(a.label[r]) ? 0 : 1;
+  for (int r0 = begin + (int)threadIdx.x; r0 < end; r0 += AT_ONCE * blockDim.x) {
+    int label[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; k++) label[k] = a.label[min(r0 + k * (int)blockDim.x, end - 1)];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; k++) n += r0 + k * (int)blockDim.x < end && !a.masked(label[k]) ? 1 : 0;
+  }
   return block_count(n, red);
 }
 // ---- rows.  Both kernels below go over the rows r = first, first + step, ...; the threads of a row ("team") are t = 0 .. TPR - 1.  Vectors of a row are those that
@@ -427,6 +433,22 @@ __device__ __forceinline__ void masked_row(const PolicyArgs& p, const SeqRows& o
   else if (p.logp) p.logp[r] = 0.f;
 }
 
+// what follows from a row's statistics: added to the sums, and what its gradient is made of (zeros before)
+template <Mode MODE>
+__device__ __forceinline__ RowStat row_result(const PolicyArgs& p, const RunPair& run, const RowInputs& in, double* sum, RowGrad& b) {
+  const RowStat s = row_stat(run.x, in.xa);
+  b.m = s.m;
+  if (MODE != STATS) policy_row(p, s, sum, in.old, in.adv, in.ref, in.w, b);
+  if (MODE == POLICY_FULL)
+    full_kl(p, s, (double)run.kl * s.by, ((double)s.m - (double)run.y.m) + (log_d(s.s) - log_d((double)run.y.s)), sum, in.xa, in.ya, in.w, b);
+  return s;
+}
+template <Mode MODE>
+__device__ __forceinline__ void row_out(const PolicyArgs& p, const SeqRows& o, int r, const RowStat& s) {
+  if (MODE == STATS) stat_row(o, r, s);
+  else if (p.logp) p.logp[r] = (float)s.lp;
+}
+
 // Adds up a row's statistics over its waves and says what follows from them, in every thread; sums: this team's
 template <int W, Mode MODE>
 __device__ __forceinline__ RowGrad row_scalars(const PolicyArgs& p, const SeqRows& o, int r, RunPair run, const RowInputs& in, RunPair* red, RowGrad* said,
@@ -445,16 +467,11 @@ __device__ __forceinline__ RowGrad row_scalars(const PolicyArgs& p, const SeqRow
       if (threadIdx.x < W) run = red[threadIdx.x];
       run.over_lanes<FULL, W>();
     }
-    const RowStat s = row_stat(run.x, in.xa);
-    b.m = s.m;
-    if (MODE == STATS) {
-      if (first) stat_row(o, r, s);
-    } else {
-      double sum[4] = {0, 0, 0, 0};
-      policy_row(p, s, sum, in.old, in.adv, in.ref, in.w, b);
-      if (FULL) full_kl(p, s, (double)run.kl * s.by, ((double)s.m - (double)run.y.m) + (log_d(s.s) - log_d((double)run.y.s)), sum, in.xa, in.ya, in.w, b);
-      if (first) {
-        if (p.logp) p.logp[r] = (float)s.lp;
+    double sum[4] = {0, 0, 0, 0};
+    const RowStat s = row_result<MODE>(p, run, in, sum, b);
+    if (first) {
+      row_out<MODE>(p, o, r, s);
+      if (MODE != STATS) {
 #pragma unroll
         for (int i = 0; i < 4; i++) sums[i] += sum[i];
         sums[4] += 1;
@@ -607,12 +624,136 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
   }
   if (MODE != STATS) {
     __syncthreads();
-    if (threadIdx.x < TEAMS * COLUMNS) parts[blockIdx.x * TEAMS * COLUMNS + threadIdx.x] = sums[threadIdx.x / COLUMNS][threadIdx.x % COLUMNS];
+    if (threadIdx.x < COLUMNS) {
+      double sum = sums[0][threadIdx.x];
+#pragma unroll
+      for (int i = 1; i < TEAMS; i++) sum += sums[i][threadIdx.x];
+      parts[blockIdx.x * COLUMNS + threadIdx.x] = sum;
+    }
+  }
+}
+
+// Short rows: a wave takes ROWS of them at a time, which stay in registers, and the scalars of all of them are worked out at once, a row in each of its first lanes (in the
+// kernel above they are most of such a row's instructions).
+constexpr int GROUP_ROWS = 4, GROUP_VECS = 2;
+template <typename T, typename G, int ROWS, int NV, Mode MODE, bool GRAD>
+__global__ __launch_bounds__(256, 4) void group_kernel(RowArgs a, PolicyArgs p, Sequences seq, SeqRows o, const int* __restrict__ counts, int n_counts,
+                                                       double* __restrict__ parts) {
+  constexpr int N = Vec<T>::N;
+  constexpr bool FULL = MODE == POLICY_FULL;
+  __shared__ int red_n[4];
+  __shared__ double sums[4][COLUMNS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  double unit = 0, sum[4] = {0, 0, 0, 0}, seen = 0;
+  if (MODE != STATS && !p.weight) unit = GRAD ? unit_weight(a, counts, n_counts, red_n) : 1.0;
+  const int begin = MODE == STATS ? seq.at(0) : 0, end = MODE == STATS ? seq.at(seq.n) : a.rows;
+  for (long long first = (long long)wave * ROWS; first < a.rows; first += (long long)gridDim.x * 4 * ROWS) {
+    const int r0 = (int)first, mine = min(r0 + lane, a.rows - 1);
+    const bool there = lane < ROWS && r0 + lane < a.rows;
+    int label = there && mine >= begin && mine < end ? a.label[mine] : -1;
+    const bool look = !a.masked(label);
+    if (!look) label = -1;
+    RowInputs in = {0, 0, 0, 0, 0, 0};
+    if (look) in = row_inputs<T, MODE>(a, p, mine, label, unit);
+    u32x4 x[ROWS][NV], y[FULL ? ROWS : 1][NV];
+    float xe[ROWS], ye[ROWS];
+    int at[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; i++) {
+      at[i] = __builtin_amdgcn_readlane(label, i);
+      const int r = min(r0 + i, a.rows - 1);
+      const T *rx = (const T*)a.logits + (long long)r * a.ld, *ry = FULL ? (const T*)p.ref + (long long)r * p.ref_ld : rx;
+      const RowShape<T, 1> s(a.classes, rx, lane);
+      const int bytes = a.masked(at[i]) ? 0 : s.Cv * (int)sizeof(T);   // (beyond the row, and of a masked one, nothing is asked for)
+      const auto sx = __builtin_amdgcn_make_buffer_rsrc((void*)(rx + s.head), 0, bytes, 0x00027000), sy = __builtin_amdgcn_make_buffer_rsrc((void*)(ry + s.head), 0, bytes, 0x00027000);
+#pragma unroll
+      for (int v = 0; v < NV; v++) {
+        x[i][v] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(sx, lane * 16, v * 64 * 16, 0));
+        if (FULL) y[i][v] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(sy, lane * 16, v * 64 * 16, 0));
+      }
+      xe[i] = ye[i] = 0.f;
+      if (!a.masked(at[i]) && lane < s.edge) {
+        xe[i] = (float)rx[s.edge_at(lane)];
+        if (FULL) ye[i] = (float)ry[s.edge_at(lane)];
+      }
+    }
+    RunPair of_mine;
+    of_mine.start();
+#pragma unroll
+    for (int i = 0; i < ROWS; i++) {
+      const RowShape<T, 1> s(a.classes, (const T*)a.logits + (long long)min(r0 + i, a.rows - 1) * a.ld, lane);
+      const LabelAt place(s, at[i]);
+      RunPair run;
+      run.start();
+#pragma unroll
+      for (int v = 0; v < NV; v++)
+        if (v < s.mine) {
+          if (v == place.v && lane == place.t) take_out<T>(x[i][v], place.k);
+          float f[N], g[N];
+          unpack<T>(x[i][v], f);
+          if (FULL) unpack<T>(y[i][v], g);
+          run.add<FULL>(f, g);
+        }
+      if (place.v < 0 && lane == place.t) xe[i] = -INFINITY;
+      if (lane < s.edge) {
+        const float f[1] = {xe[i]}, g[1] = {ye[i]};
+        run.add<FULL>(f, g);
+      }
+      run.over_lanes<FULL, 64>();
+      if (lane == i) of_mine = run;
+    }
+    RowGrad b = {0.f, 0.f, 0.f, 0.f, 0.f};
+    if (look) {
+      row_out<MODE>(p, o, mine, row_result<MODE>(p, of_mine, in, sum, b));
+      seen += 1;
+    } else if (there) {
+      masked_row<MODE>(p, o, mine);
+    }
+    if (!GRAD) continue;
+#pragma unroll
+    for (int i = 0; i < ROWS; i++) {
+      if (r0 + i >= a.rows) break;
+      auto of = [&](float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), i)); };
+      const RowGrad c = {of(b.m), of(b.cf), of(b.ck), of(b.kk), of(b.own)};
+      const RowShape<T, 1> s(a.classes, (const T*)a.logits + (long long)(r0 + i) * a.ld, lane);
+      const LabelAt place(s, at[i]);
+      G* const out = (G*)a.grad + (long long)(r0 + i) * a.gld;
+#pragma unroll
+      for (int v = 0; v < NV; v++)
+        if (v < s.mine) {
+          float f[N], g[N], d[N];
+          unpack<T>(x[i][v], f);
+          if (FULL) unpack<T>(y[i][v], g);
+          gradient<FULL>(c, f, g, d);
+#pragma unroll
+          for (int k = 0; k < N; k++) d[k] = v == place.v && lane == place.t && k == place.k ? c.own : d[k];
+          store_vec(out + s.head + (v * 64 + lane) * N, d);
+        }
+      if (lane < s.edge) {
+        const float f[1] = {xe[i]}, g[1] = {ye[i]};
+        float d[1];
+        gradient<FULL>(c, f, g, d);
+        out[s.edge_at(lane)] = (G)(place.v == -1 && lane == place.t ? c.own : d[0]);
+      }
+    }
+  }
+  if (MODE != STATS) {
+    double line[COLUMNS] = {sum[0], sum[1], sum[2], sum[3], seen};
+#pragma unroll
+    for (int i = 0; i < COLUMNS; i++) {
+#pragma unroll
+      for (int d = 1; d < ROWS; d *= 2) line[i] += __shfl_xor(line[i], d, 64);
+      if (lane == 0) sums[threadIdx.x >> 6][i] = line[i];
+    }
+    __syncthreads();
+    if (threadIdx.x < COLUMNS) parts[blockIdx.x * COLUMNS + threadIdx.x] = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
   }
 }
 
 // Rows of any length, streamed through a window of U vectors a thread: as each has been used the vector U further on is loaded in its place.  Where there is a gradient
-// the row passes twice, and the beginning of the second pass is on the way before the first has ended.
+// the row passes twice, and the beginning of the second pass is on the way before the first has ended.  That second pass finds the row in the last-level cache: sixteen waves a row leave
+// one on a compute unit at a time, and the gradient goes past the cache (2197 rows of 96785 float32 classes: 385 us, 4.4 TB/s counting logits and gradient once; with stores through the
+// cache 411, with rows of four waves, four on a compute unit, 525).
 template <typename T, typename G, int W, int U, Mode MODE, bool GRAD, bool NT>
 __global__ __launch_bounds__(64 * W, 4) void streamed_kernel(RowArgs a, PolicyArgs p, Sequences seq, SeqRows o, const int* __restrict__ counts, int n_counts,
                                                              double* __restrict__ parts) {
@@ -698,7 +839,7 @@ __global__ __launch_bounds__(64 * W, 4) void streamed_kernel(RowArgs a, PolicyAr
 #pragma unroll
               for (int k = 0; k < N; k++) d[k] = k == place.k ? b.own : d[k];
           }
-          store_vec<G>(out + shape.head + (size_t)(v + i) * (TPR * N) + t * N, d);
+          store_vec<G, true>(out + shape.head + (size_t)(v + i) * (TPR * N) + t * N, d);
         }
         fetch(v + U, i);
       }
@@ -721,11 +862,14 @@ struct RowPlan {
   bool keep;
   int groups;
   bool nt;
+  int rows = 1;   // of a wave at a time
   int teams() const { return waves == 1 ? 4 : 1; }
 };
 // Sixteen vectors a thread (of both rows together) and sixteen waves on a compute unit are what its registers hold.  Where nothing is written rows need not stay: they are
 // streamed, a workgroup each, more of them at once than run, so that none has much more of them than another (2048 rows of 32000 classes of which one in five is
 // masked take 26.8 us, over the workgroups that run at once 28.3).
+// Short rows are taken four at a time where there are more than run at once (16384 rows of 200 bf16 classes 20.3 us, one at a time 24.2; 4096 of 1000 14.1 and 13.1; exact divergence of
+// 16384 rows of 200 float32 24.3 and 26.8, but of 1000 bf16, twice the vectors, 38.9 and 37.3).
 // A row that a wave's registers hold takes one (16384 rows of 4000 bf16 classes 59 us, with four waves 88).
 // Rows no more than compute units leave them idle, so such a row takes more waves: four from a half of a wave's registers on (64 rows of 4000 8.5 us instead of 9.9); with a
 // gradient eight from 1024 vectors on (256 rows of 32000 13.9 us instead of 15.4; below, 64 rows of 8000 take 9.1 with four and 9.4 with eight); without one sixteen from 2048 on
@@ -738,6 +882,7 @@ inline RowPlan row_plan(int rows, int classes, size_t size, bool full, bool grad
   const int64_t vecs = ((int64_t)classes * (int64_t)size + 15) / 16, most = full ? 8 : 16, alone = 64 * (full ? 4 : 8);
   const double bytes = (double)rows * classes * size;
   const bool few = rows <= cus;
+  if (vecs <= 64 * GROUP_VECS / (full ? 2 : 1) && rows > 16 * cus) return {1, true, 4 * cus, false, GROUP_ROWS};
   if (vecs <= (few ? alone / 2 : alone)) return {1, true, 4 * cus, false};
   const bool nt = bytes > CACHED;
   if (!grad) return {few && vecs > 2048 ? 16 : 4, false, MAX_GRID, !again || nt};
@@ -745,9 +890,9 @@ inline RowPlan row_plan(int rows, int classes, size_t size, bool full, bool grad
   if (vecs <= 256 * most) return {4, true, 4 * cus, nt};
   if (vecs <= 512 * most) return {8, true, 2 * cus, nt};
   if (vecs <= 1024 * most) return {16, true, cus, nt};
-  return {4, false, MAX_GRID, false};
+  return {16, false, MAX_GRID, false};
 }
-inline int row_grid(int rows, const RowPlan& plan) { return std::min(std::min(MAX_GRID, plan.groups), (rows - 1) / plan.teams() + 1); }
+inline int row_grid(int rows, const RowPlan& plan) { return std::min(std::min(MAX_GRID, plan.groups), (rows - 1) / (plan.teams() * plan.rows) + 1); }
 
 struct RowCall {
   RowArgs a;
@@ -764,17 +909,17 @@ void row_launch(const RowPlan& plan, int grid, hipStream_t s, const RowCall& c) 
 #define ET_ROW(KERNEL, W, NV, NT) \
   hipLaunchKernelGGL((KERNEL<T, G, W, NV, MODE, GRAD, NT>), dim3(grid), dim3(W == 1 ? 256 : 64 * W), 0, s, c.a, c.p, c.seq, c.o, c.counts, c.n_counts, c.parts)
   constexpr bool SAME = std::is_same<T, G>::value;   // (a gradient of another type than the logits is rare: not both kinds of kernels)
-  if (plan.waves == 1) {
-    // (16384 rows of 200 bf16 classes 26.9 us, as the first part of eight vectors 28.5)
-    if (c.a.classes * sizeof(T) <= 64 * 16 * 2) ET_ROW(kept_kernel, 1, 2, false);
-    else ET_ROW(kept_kernel, 1, 8 / F, false);
+  if (plan.rows > 1) {
+    hipLaunchKernelGGL((group_kernel<T, G, GROUP_ROWS, GROUP_VECS, MODE, GRAD>), dim3(grid), dim3(256), 0, s, c.a, c.p, c.seq, c.o, c.counts, c.n_counts, c.parts);
+  } else if (plan.waves == 1) {
+    ET_ROW(kept_kernel, 1, 8 / F, false);
   } else if constexpr (!GRAD) {
     if (plan.waves == 16 && plan.nt) ET_ROW(streamed_kernel, 16, 8 / F, true);
     else if (plan.waves == 16) ET_ROW(streamed_kernel, 16, 8 / F, false);
     else if (plan.nt) ET_ROW(streamed_kernel, 4, 8 / F, true);
     else ET_ROW(streamed_kernel, 4, 8 / F, false);
   } else if (!plan.keep) {
-    ET_ROW(streamed_kernel, 4, 8 / F, false);
+    ET_ROW(streamed_kernel, 16, 8 / F, false);
   } else if (plan.nt && SAME) {
     if (plan.waves == 4) ET_ROW(kept_kernel, 4, 16 / F, SAME);
     else if (plan.waves == 8) ET_ROW(kept_kernel, 8, 16 / F, SAME);

@@ -9,15 +9,6 @@ namespace et {
 namespace rows {
 namespace {
 
-__device__ __forceinline__ double block_sum_d(double v, double* red) {   // 256 threads
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
-}
-
 __global__ __launch_bounds__(256) void count_kernel(RowArgs a, int* __restrict__ counts) {
   __shared__ int red[4];
   const long long per = ((long long)a.rows + gridDim.x - 1) / gridDim.x;
@@ -174,25 +165,28 @@ __global__ __launch_bounds__(256) void pair_rows_kernel(RowArgs a, PairArgs q, d
   }
 }
 
+// A workgroup a pair, a half of it a sequence: the sums of its rows, eight a thread at once, then the rows' factors
 __global__ __launch_bounds__(256) void pair_kernel(Sequences seq, SeqRows o, PairArgs q, double* __restrict__ parts) {
+  constexpr int AT_ONCE = 8;
   __shared__ double red[4];
-  const int pair = blockIdx.x;
-  double L[2];
+  const int pair = blockIdx.x, i = threadIdx.x >> 7, t = threadIdx.x & 127;
+  const int begin = seq.at(2 * pair + i), end = seq.at(2 * pair + i + 1);
+  double v = 0;
+  for (int r0 = begin + t; r0 < end; r0 += AT_ONCE * 128) {
+    double lp[AT_ONCE];
 #pragma unroll
-  for (int i = 0; i < 2; i++) {
-    const int begin = seq.at(2 * pair + i), end = seq.at(2 * pair + i + 1);
-    double v = 0;
-    for (int r = begin + (int)threadIdx.x; r < end; r += 256) v += o.lp[r];
-    L[i] = block_sum_d(v, red);
-    if (q.logp && threadIdx.x == 0) q.logp[2 * pair + i] = (float)L[i];
+    for (int k = 0; k < AT_ONCE; k++) lp[k] = o.lp[min(r0 + k * 128, end - 1)];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; k++) v += r0 + k * 128 < end ? lp[k] : 0.0;
   }
-  const double z = pair_margin(q, pair, L[0], L[1]);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  const double L0 = red[0] + red[1], L1 = red[2] + red[3], z = pair_margin(q, pair, L0, L1);
   const float g = pair_factor(q, z);
-#pragma unroll
-  for (int i = 0; i < 2; i++) {
-    const int begin = seq.at(2 * pair + i), end = seq.at(2 * pair + i + 1);
-    for (int r = begin + (int)threadIdx.x; r < end; r += 256) o.g[r] = i == 0 ? g : -g;
-  }
+  for (int r = begin + t; r < end; r += 128) o.g[r] = i == 0 ? g : -g;
+  if (t == 0 && q.logp) q.logp[2 * pair + i] = (float)(i == 0 ? L0 : L1);
   if (threadIdx.x == 0) {
     parts[3 * pair] = pair_loss(q, z);
     parts[3 * pair + 1] = z;
@@ -252,7 +246,7 @@ namespace {
 using namespace et_op;
 
 constexpr int MAX_COUNTS = 256;
-constexpr size_t POLICY_WS = sizeof(int) * MAX_COUNTS + sizeof(double) * et::rows::COLUMNS * 4 * et::rows::MAX_GRID;
+constexpr size_t POLICY_WS = sizeof(int) * MAX_COUNTS + sizeof(double) * et::rows::COLUMNS * et::rows::MAX_GRID;
 
 constexpr int MOST_PAIRS = 1 << 23;   // (a workgroup each: what a launch can have)
 size_t preference_ws(int64_t rows, int64_t pairs) { return (size_t)(rows * 24 + pairs * 24 + 256); }
@@ -306,18 +300,17 @@ int et_op::policy_loss(int32_t rows, int32_t classes, const void* logits_dev, in
   const et::rows::RowPlan plan = et::rows::row_plan(rows, classes, type_size(dtype), c.p.ref != nullptr, grad_dev != nullptr, false, device_cus(on.dev));
   const int grid = et::rows::row_grid(rows, plan);
   if (grad_dev && !p->weight_dev && rows > et::rows::COUNT_ROWS) {
-    c.n_counts = std::min(MAX_COUNTS, rows / 4096);
+    c.n_counts = std::min(MAX_COUNTS, rows / 1024);
     hipLaunchKernelGGL(et::rows::count_kernel, dim3(c.n_counts), dim3(256), 0, s, c.a, counts);
   }
   if (dtype == ET_BF16) et::rows::rows_of_policy<bf16>(plan, grid, s, c, grad_dtype == ET_BF16);
   else et::rows::rows_of_policy<float>(plan, grid, s, c, grad_dtype == ET_BF16);
   if (launches) *launches = 2 + (c.n_counts != 0);
   // (without a gradient rows have the weight 1 as they are added up)
-  const int lines = grid * plan.teams();
   if (!grad_dev && !p->weight_dev)
-    et::rows::finish_launch<et::rows::COLUMNS, 4>(s, c.parts, lines, 1.0, loss_dev, p->stats_dev, 3);
+    et::rows::finish_launch<et::rows::COLUMNS, 4>(s, c.parts, grid, 1.0, loss_dev, p->stats_dev, 3);
   else
-    et::rows::finish_launch<et::rows::COLUMNS, -1>(s, c.parts, lines, 1.0, loss_dev, p->stats_dev, 3);
+    et::rows::finish_launch<et::rows::COLUMNS, -1>(s, c.parts, grid, 1.0, loss_dev, p->stats_dev, 3);
   return hipGetLastError() == hipSuccess ? ET_OK : ET_EHIP;
 }
 

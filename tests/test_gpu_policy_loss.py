@@ -363,3 +363,40 @@ def test_a_class_that_the_reference_gives_probability_zero(C, bf16):
     w = c.want()["grad"]
     c.y[1, 9] = kept
     assert np.abs(g[[0, 2, 3]] - w[[0, 2, 3]]).max() <= 2 * half_step(bf16) * np.abs(w).max() + 1e-5 * np.abs(w).max()
+
+
+@pytest.mark.parametrize("kl", ["none", "sampled", "full"])
+@pytest.mark.parametrize("rows,C,bf16,kw", [(4100, 1000, True, {}), (4097, 512, False, dict(weighted=True)), (5001, 1, True, {}), (4500, 130, True, dict(in_place=True, stride=133, skip=1)),
+                                            (4300, 220, False, dict(gbf16=True, gstride=301, gskip=3)), (4300, 510, True, dict(gbf16=False, stride=1030, skip=5)),
+                                            (9000, 77, False, dict(train=False)), (4099, 255, False, dict(masked=0.9)), (2100, 1000, True, {})])
+def test_many_short_rows(rows, C, bf16, kw, kl):
+    Case(rows, C, bf16, kl, seed=6, **kw).call().check()
+
+
+@pytest.mark.parametrize("kl", ["sampled", "full"])
+def test_many_short_rows_give_what_few_do(kl):
+    """Rows with masks, nothing, NaN and huge values among many: every row's outputs as from a call of a few."""
+    def edit(c):
+        rng = np.random.default_rng(1)
+        c.x[5::50] = -np.inf
+        c.x[6::50][rng.random(c.x[6::50].shape) < 0.7] = -np.inf
+        c.y[6::50] = c.x[6::50]
+        c.x[7::50] *= 8.0
+        c.x[8::50, 0] = np.nan
+
+    c = Case(4500, 201, True, kl, seed=7, weighted=True, edit=edit).call()
+    g, lp = c.grad.host(), c.logp.cpu().numpy()
+    rows = 1000
+    for at in range(0, 4500, rows):
+        n = min(rows, 4500 - at)
+        part = Case(n, 201, True, kl, seed=8, weighted=True, masked=0)
+        for name in ("x", "y", "label", "old", "adv", "ref", "weight"):
+            setattr(part, name, getattr(c, name)[at:at + n])
+        part.logits.put(round_to(part.x, True)), part.refs.put(round_to(part.y, True))
+        part.d = {k: dev(getattr(part, k)) for k in ("old", "adv", "ref", "weight")}
+        part.d["label"] = dev(part.label, np.int32)
+        part.call()
+        # (two kernels may contract their products differently: a step of the type, and of float32 some)
+        np.testing.assert_allclose(part.grad.host(), g[at:at + n], rtol=2.0 ** -7, atol=1e-12)
+        np.testing.assert_allclose(part.logp.cpu().numpy(), lp[at:at + n], rtol=1e-5, atol=1e-6)
+    assert np.isnan(g[8::50]).any() and not np.isnan(g[9::50]).any()

@@ -322,3 +322,8 @@ def test_more_logits_than_the_caches_hold(rows, C, bf16):
     for at in (0, rows // 2):
         run(1, at, rows // 2, 2)
     assert torch.equal(logp[0], logp[1]) and torch.equal(grads[0] * 2, grads[1])
+
+
+@pytest.mark.parametrize("C,bf16,kw", [(600, True, {}), (77, False, dict(gbf16=True, pad=3, skip=1)), (512, False, dict(in_place=True)), (1024, True, dict(train=False))])
+def test_many_short_rows(C, bf16, kw):
+    Case([1700, 0, 1, 1900, 500, 400], C, bf16, front=1, behind=3, beta=0.01, **kw).call().check()
