@@ -912,7 +912,9 @@ void row_launch(const RowPlan& plan, int grid, hipStream_t s, const RowCall& c) 
   if (plan.rows > 1) {
     hipLaunchKernelGGL((group_kernel<T, G, GROUP_ROWS, GROUP_VECS, MODE, GRAD>), dim3(grid), dim3(256), 0, s, c.a, c.p, c.seq, c.o, c.counts, c.n_counts, c.parts);
   } else if (plan.waves == 1) {
-    ET_ROW(kept_kernel, 1, 8 / F, false);
+    // (4096 rows of 200 bf16 classes 10.9 us, as the first part of eight vectors 11.6)
+    if (c.a.classes * sizeof(T) <= 64 * 16 * 2) ET_ROW(kept_kernel, 1, 2, false);
+    else ET_ROW(kept_kernel, 1, 8 / F, false);
   } else if constexpr (!GRAD) {
     if (plan.waves == 16 && plan.nt) ET_ROW(streamed_kernel, 16, 8 / F, true);
     else if (plan.waves == 16) ET_ROW(streamed_kernel, 16, 8 / F, false);
