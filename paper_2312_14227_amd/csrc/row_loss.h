@@ -6,7 +6,7 @@
 //
 // What bounds them: memory, with the vector units close behind.  An element costs a row's statistics some 8 issue slots, four of them the exponential, and the
 // gradient 8 more: by count, a row of 128000 bf16 classes takes a compute unit 18 us of those and 24 us of its share of the memory.  Policy loss with gradient of 8192 such rows:
-// 813 us, 5.2 TB/s; its value alone of 2048 rows of 32000, one in five masked: 26.8 us, 3.9 TB/s; exact divergence of 4096 rows of 50257, one in ten masked: 264 us, 4.4 TB/s.
+// 813 us, 5.2 TB/s; its value alone of 2048 rows of 32000, one in five masked: 25.4 us, 4.1 TB/s; exact divergence of 4096 rows of 50257, one in ten masked: 263 us, 4.4 TB/s.
 #pragma once
 #include <cmath>
 #include <type_traits>
@@ -867,14 +867,14 @@ struct RowPlan {
 };
 // Sixteen vectors a thread (of both rows together) and sixteen waves on a compute unit are what its registers hold.  Where nothing is written rows need not stay: they are
 // streamed, a workgroup each, more of them at once than run, so that none has much more of them than another (2048 rows of 32000 classes of which one in five is
-// masked take 26.8 us, over the workgroups that run at once 28.3).
+// masked take 25.4 us, over the workgroups that run at once 27.8).
 // Short rows are taken four at a time where there are more than run at once (16384 rows of 200 bf16 classes 20.3 us, one at a time 24.2; 4096 of 1000 14.1 and 13.1; exact divergence of
 // 16384 rows of 200 float32 24.3 and 26.8, but of 1000 bf16, twice the vectors, 38.9 and 37.3).
 // A row that a wave's registers hold takes one (16384 rows of 4000 bf16 classes 59 us, with four waves 88).
 // Rows no more than compute units leave them idle, so such a row takes more waves: four from a half of a wave's registers on (64 rows of 4000 8.5 us instead of 9.9); with a
 // gradient eight from 1024 vectors on (256 rows of 32000 13.9 us instead of 15.4; below, 64 rows of 8000 take 9.1 with four and 9.4 with eight); without one sixteen from 2048 on
 // (64 rows of 128000 14.5 us instead of 22.4; one row of 16400 takes 7.8 with four and 8.1 with sixteen).
-// Past the caches goes what is read once: preference loss of 7148 rows of 100003 classes 626 us instead of 656, values of 2048 rows of 32000 26.8 instead of 27.8.  What the last-level
+// Past the caches goes what is read once: preference loss of 7148 rows of 100003 classes 624 us instead of 654, values of 2048 rows of 32000 25.4 instead of 26.4.  What the last-level
 // cache holds (256 MB) until the gradient's pass or the next kernel reads it is left there: four short pairs of 32000 classes, 63 MB, would take 41.1 us instead of 35.8.  Loads and stores
 // of gradients that it cannot hold: exact divergence of 4096 rows of 50257 classes 264 us instead of 273, policy loss of 8192 of 128000 813 instead of 824.
 constexpr double CACHED = 192e6;

@@ -23,9 +23,18 @@ __device__ __forceinline__ void finish(const double* __restrict__ parts, int lin
   double v[COLS];
 #pragma unroll
   for (int i = 0; i < COLS; i++) v[i] = 0;
-  for (int l = threadIdx.x; l < lines; l += THREADS)
+  constexpr int AT_ONCE = 4;
+  for (int l0 = threadIdx.x; l0 < lines; l0 += AT_ONCE * THREADS) {
+    double line[AT_ONCE][COLS];
 #pragma unroll
-    for (int i = 0; i < COLS; i++) v[i] += parts[(size_t)COLS * l + i];
+    for (int k = 0; k < AT_ONCE; k++)
+#pragma unroll
+      for (int i = 0; i < COLS; i++) line[k][i] = parts[(size_t)COLS * min(l0 + k * THREADS, lines - 1) + i];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; k++)
+#pragma unroll
+      for (int i = 0; i < COLS; i++) v[i] += l0 + k * THREADS < lines ? line[k][i] : 0.0;
+  }
 #pragma unroll
   for (int i = 0; i < COLS; i++) {
 #pragma unroll
@@ -48,10 +57,10 @@ __global__ __launch_bounds__(THREADS) void finish_kernel(const double* __restric
                                                          int n_more) {
   finish<THREADS, COLS, OF>(parts, lines, scale, out, more, n_more);
 }
-// (64 lines: 0.9 us less with 256 threads than with 1024; 1000 lines: 0.2 less; 8000: 4.7 more)
+// (2048 lines of workgroups' sums: 256 threads take 1.4 us less than 1024; 4096: 0.4 less; 8000 of pairs': 0.9 more)
 template <int COLS, int OF>
 void finish_launch(hipStream_t s, const double* parts, int lines, double scale, float* out, float* more, int n_more) {
-  if (lines <= 1024) hipLaunchKernelGGL((finish_kernel<256, COLS, OF>), dim3(1), dim3(256), 0, s, parts, lines, scale, out, more, n_more);
+  if (lines <= 4096) hipLaunchKernelGGL((finish_kernel<256, COLS, OF>), dim3(1), dim3(256), 0, s, parts, lines, scale, out, more, n_more);
   else hipLaunchKernelGGL((finish_kernel<1024, COLS, OF>), dim3(1), dim3(1024), 0, s, parts, lines, scale, out, more, n_more);
 }
 
@@ -74,8 +83,8 @@ __device__ __forceinline__ double pair_margin(const PairArgs& q, int pair, doubl
   return q.beta * ((chosen - (q.ref ? (double)q.ref[2 * pair] : 0.0)) - (other - (q.ref ? (double)q.ref[2 * pair + 1] : 0.0)));
 }
 
-// Pairs of single rows, a wave each: both rows stay in registers.  One pass and two launches instead of two passes and three: 32 pairs of 200 bf16 classes 7.3 us instead of 9.4,
-// 8000 pairs 18.7 instead of 39.7, 1000 pairs of 2000 classes 12.0 instead of 14.0.
+// Pairs of single rows, a wave each: both rows stay in registers.  One pass and two launches instead of two passes and three: 32 pairs of 200 bf16 classes 7.4 us instead of 9.0,
+// 8000 pairs 17.6 instead of 27.7, 1000 pairs of 2000 classes 11.3 instead of 13.0.
 constexpr int PAIR_VECS = 4;
 bool pair_rows_fit(int classes, size_t size) { return (int64_t)classes * (int64_t)size <= 64 * 16 * PAIR_VECS; }
 template <typename T, typename G>
