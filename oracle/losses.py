@@ -61,7 +61,10 @@ def preference_loss(logits, label, offsets, beta, label_smoothing=0.0, ref_logp=
     far = L - (np.asarray(ref_logp, np.float64) if ref_logp is not None else 0.0)
     z = beta * (far[0::2] - far[1::2])
     sigma = lambda v: 1.0 / (1.0 + np.exp(-v))  # noqa: E731
-    loss = (1 - label_smoothing) * np.logaddexp(0, -z) + label_smoothing * np.logaddexp(0, z)
+    loss = np.zeros(pairs)                                     # (what has no weight counts for nothing, were it infinite)
+    for share, v in ((1 - label_smoothing, -z), (label_smoothing, z)):
+        if share != 0:
+            loss += share * np.logaddexp(0, v)
     dz = label_smoothing * sigma(z) - (1 - label_smoothing) * sigma(-z)
     for i in range(2 * pairs):
         grad[offsets[i]:offsets[i + 1]] *= (1 if i % 2 == 0 else -1) * beta * dz[i // 2] / pairs
