@@ -70,7 +70,8 @@ struct PairArgs {
   double beta, eps, per_pair;
   float* logp;
 };
-__device__ __forceinline__ double softplus(double x) { return x == INFINITY ? x : (x > 0 ? x : 0.0 * x) + log1p_d(exp_d(-fabs(x))); }
+// log(1 + exp x): infinity of infinity, 0 of minus infinity, and NaN of NaN (which no comparison picks)
+__device__ __forceinline__ double softplus(double x) { return x == INFINITY ? x : (x <= 0 ? 0.0 : x) + log1p_d(exp_d(-fabs(x))); }
 // of a pair's margin: the factor of its gradient, and its loss
 __device__ __forceinline__ float pair_factor(const PairArgs& q, double z) {
   const double up = 1.0 / (1.0 + exp_d(-z)), down = 1.0 / (1.0 + exp_d(z));
