@@ -309,7 +309,7 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& p, const RowStat& s
   if (p.ref_logp) {
     const double d = (double)ref - s.lp;
     kl = exp_rest(d);
-    if (p.kl_coef != 0) g -= p.kl_coef * (kl + d);
+    if (p.kl_coef != 0) g -= p.kl_coef * (d == -INFINITY ? -1.0 : kl + d);   // exp(d) - 1
   }
   sum[0] += w * ((p.kl_coef != 0 ? p.kl_coef * kl : 0.0) - surrogate);
   sum[1] += w * surrogate;

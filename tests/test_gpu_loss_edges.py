@@ -32,3 +32,15 @@ def test_an_infinite_margin(C, offsets, row, eps):
     assert c.logp[row].item() == -np.inf
     p = np.exp([losses.log_softmax(v) for v in c.x])
     close(c.grad.host(), w["grad"], half_step(False) * np.abs(w["grad"]) + R * c.beta / 2 * (1 + size) * np.maximum(p, np.arange(C) == 2) + 1e-37, "grad")
+
+
+@pytest.mark.parametrize("rows,C,bf16,kw", [(9, 200, False, {}), (9, 6000, True, {}), (9, 140001, True, {}), (4500, 40, True, {}), (9, 200, True, dict(train=False)),
+                                            (9, 5001, True, dict(in_place=True))])
+def test_a_reference_that_gives_the_label_probability_zero(rows, C, bf16, kw):
+    """exp(d) - d - 1 at d = -infinity is infinite, and its slope along d is -1."""
+    def edit(c):
+        c.label[1:3] = 0
+        c.ref[1] = -np.inf
+
+    c = Policy(rows, C, bf16, edit=edit, **kw).call().check()
+    assert c.loss.item() == np.inf and (not c.grad or np.isfinite(c.grad.host()).all())
