@@ -318,17 +318,18 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& p, const RowStat& s
   o.cf = (float)(-w * g * s.inv_s);
   o.own = (float)(w * g * (s.rest * s.inv_s));
 }
-// the exact divergence on top; log_ratio: log sum exp x - log sum exp y
+// the exact divergence on top; log_ratio: log sum exp x - log sum exp y, NaN where the reference has no distribution: then the divergence is, and with it every element of the gradient
+// (the differences alone do not show it: what is not a number among them counts for something finite)
 __device__ __forceinline__ void full_kl(const PolicyArgs& p, const RowStat& s, double sum_apart, double log_ratio, double* sum, float xa, float ya, double w, RowGrad& o) {
   if (s.none) return;
   const double mine = (double)apart(xa, ya), kk = (sum_apart + (s.ea == 0 ? 0.0 : s.ea * mine)) * s.inv_s;
-  const double kl = kk - log_ratio;
+  const double kl = kk - log_ratio, nan = kl - kl;   // (0 otherwise)
   sum[2] += w * kl;
   if (p.kl_coef == 0) return;
   sum[0] += w * p.kl_coef * kl;
-  o.kk = (float)kk;
+  o.kk = (float)(kk + nan);
   o.ck = (float)(w * p.kl_coef * s.inv_s);
-  if (s.ea != 0) o.own = (float)((double)o.own + w * p.kl_coef * (s.ea * s.inv_s) * (mine - kk));
+  o.own = (float)((double)o.own + nan + (s.ea != 0 ? w * p.kl_coef * (s.ea * s.inv_s) * (mine - kk) : 0.0));
 }
 
 constexpr int AUX_NT = 2;   // cache policy of a buffer load: non-temporal
@@ -440,7 +441,7 @@ __device__ __forceinline__ RowStat row_result(const PolicyArgs& p, const RunPair
   b.m = s.m;
   if (MODE != STATS) policy_row(p, s, sum, in.old, in.adv, in.ref, in.w, b);
   if (MODE == POLICY_FULL)
-    full_kl(p, s, (double)run.kl * s.by, ((double)s.m - (double)run.y.m) + (log_d(s.s) - log_d((double)run.y.s)), sum, in.xa, in.ya, in.w, b);
+    full_kl(p, s, (double)run.kl * s.by, run.y.s == 0.f ? NAN : ((double)s.m - (double)run.y.m) + (log_d(s.s) - log_d((double)run.y.s)), sum, in.xa, in.ya, in.w, b);
   return s;
 }
 template <Mode MODE>

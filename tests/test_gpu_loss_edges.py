@@ -44,3 +44,57 @@ def test_a_reference_that_gives_the_label_probability_zero(rows, C, bf16, kw):
 
     c = Policy(rows, C, bf16, edit=edit, **kw).call().check()
     assert c.loss.item() == np.inf and (not c.grad or np.isfinite(c.grad.host()).all())
+
+
+def _shifted(c, w):
+    """Bounds of the gradient with the exact divergence: what a difference x - y is off by is relative to how far both lie below their row's maxima."""
+    R, n = 4 * rel(c.C), ((c.label >= 0) & (c.label < c.C)).sum()
+    bound, kl_size, size = np.zeros_like(c.x), np.zeros(c.rows), np.zeros(c.rows)
+    for r in range(c.rows):
+        if 0 <= c.label[r] < c.C and np.isfinite(w["grad"][r]).all():
+            lp = losses.log_softmax(c.x[r])
+            p = np.exp(lp)
+            far = 1 + 3 * ((c.x[r].max() - c.x[r]) + (c.y[r].max() - c.y[r]))[p > 0].max()
+            size[r] = (1 + abs(lp[c.label[r]])) * abs(c.adv[r]) * (1 + np.exp(lp[c.label[r]] - c.old[r]))
+            kl_size[r] = KL * far
+            bound[r] = half_step(c.gbf16) * np.abs(w["grad"][r]) + R / n * ((size[r] + kl_size[r]) * p + size[r] * (np.arange(c.C) == c.label[r])) + 1e-37
+    return bound, R / n * (size + kl_size)
+
+
+REFERENCES = [(6, 200, False, {}), (6, 200, True, dict(in_place=True)), (6, 6000, True, {}), (6, 70001, False, {}), (6, 140001, True, {}), (4500, 100, True, {}),
+              (6, 200, True, dict(train=False)), (6, 40001, True, dict(train=False))]
+
+
+@pytest.mark.parametrize("rows,C,bf16,kw", REFERENCES)
+def test_a_reference_without_a_distribution(rows, C, bf16, kw):
+    """A reference row with NaN or plus infinity in it, or nothing but minus infinity: the row's divergence and gradient are NaN, and with them the loss; the other rows' stay."""
+    def edit(c):
+        c.label[:5] = 3
+        c.y[1, 7], c.y[2, 9], c.y[3], c.y[4, 3] = np.nan, np.inf, -np.inf, np.nan
+
+    c = Policy(rows, C, bf16, "full", edit=edit, masked=0.1 if rows > 6 else 0, **kw).call()
+    assert np.isnan(c.loss.item()) and np.isnan(c.stats[1].item()) and np.isfinite(c.stats[0].item())
+    if c.grad:
+        g = c.grad.host()
+        assert np.isnan(g[1:5]).all()
+        with np.errstate(all="ignore"):
+            w = c.want()
+        at = np.r_[0:1, 5:rows]
+        close(g[at], w["grad"][at], _shifted(c, w)[0][at], "grad")
+
+
+def test_a_reference_without_a_distribution_where_the_coefficient_is_zero(monkeypatch):
+    """The divergence is reported; the loss and the gradient are those without one."""
+    import test_gpu_policy_loss as t
+    monkeypatch.setattr(t, "KL", 0.0)
+
+    def edit(c):
+        c.y[1, 7], c.y[2], c.y[3, 5] = np.nan, -np.inf, np.inf
+
+    c = Policy(6, 300, False, "full", edit=edit, masked=0).call()
+    assert np.isnan(c.stats[1].item())
+    c.kl = "none"
+    w, R = c.want(), 4 * rel(300)
+    size = (1 + np.abs(w["logp"])) * np.abs(c.adv) * (1 + np.exp(w["logp"] - c.old)) / 6
+    close(c.loss.item(), w["loss"], R * size.sum(), "loss")
+    close(c.grad.host(), w["grad"], half_step(False) * np.abs(w["grad"]) + R * size[:, None] + 1e-37, "grad")
