@@ -176,10 +176,12 @@ struct Run {
   }
   __device__ __forceinline__ bool above(float top) const { return top > m + 11.f; }
   template <int N>
-  __device__ __forceinline__ void add(const float (&f)[N], float (&e)[N]) {   // e: the terms
+  __device__ __forceinline__ void add(const float (&f)[N], float (&d)[N], float (&e)[N]) {   // d: the distances to m, e: the terms
 #pragma unroll
-    for (int k = 0; k < N; k++) e[k] = exp_of(f[k] - m);
-    t = fmaf(e[0], fmaxf(f[0] - m, -1e4f), t);
+    for (int k = 0; k < N; k++) d[k] = f[k] - m;
+#pragma unroll
+    for (int k = 0; k < N; k++) e[k] = exp_of(d[k]);
+    t = fmaf(e[0], fmaxf(d[0], -1e4f), t);
     s0 += e[0];
     float a = e[0];
 #pragma unroll
@@ -187,12 +189,10 @@ struct Run {
     s += a;
   }
   template <int LANES>
-  __device__ __forceinline__ float over_lanes() {   // returns the lane's factor
-    const float f = raise(lanes_max<LANES>(m));
+  __device__ __forceinline__ void sum_lanes() {   // of one m
     s = lanes_sum<LANES>(s);
     s0 = lanes_sum<LANES>(s0);
     t = lanes_sum<LANES>(t);
-    return f;
   }
 };
 // (the builtin maximum would first quiet every operand, an instruction each)
@@ -208,36 +208,49 @@ __device__ __forceinline__ float max_of(const float (&f)[N]) {
   for (int k = 1; k < N; k += 2) top = max3(top, f[k], f[k + 1 < N ? k + 1 : k]);
   return top;
 }
-// x - y of two logits; minus infinity less itself, of a class that both give probability zero, counts for nothing
-__device__ __forceinline__ float apart(float x, float y) { return __builtin_amdgcn_fmed3f(x - y, -1e30f, 1e30f); }
-// Two rows at once, and kl = sum over x's terms of term * (x - y)
+// dx - dy of two logits' distances to their row's reference.  What is further apart than 1e30 counts as that far, an infinite difference too; minus infinity less itself, of a class that both
+// give probability zero, counts for nothing, as its term does
+constexpr float FARTHEST = 1e30f;
+__device__ __forceinline__ float apart(float dx, float dy) { return __builtin_amdgcn_fmed3f(dx - dy, -FARTHEST, FARTHEST); }
+// Two rows at once, and kl = sum over x's terms of term * (dx - dy): of distances, so that what a whole row has in common, be it the type's lowest value, does not count
 struct RunPair {
   Run x, y;
   float kl;
   __device__ __forceinline__ void start() { x.start(), y.start(), kl = 0.f; }
+  template <bool FULL>
+  __device__ __forceinline__ void raise_x(float to) {
+    const float by = fminf(to - x.m, 1e4f), s = x.s, f = x.raise(to);   // (beyond 1e4 nothing is left of the terms)
+    if (FULL) kl = f * fmaf(-s, by, kl);
+  }
+  __device__ __forceinline__ void raise_y(float to) {
+    if (y.s != 0.f) kl = fmaf(x.s, fminf(to - y.m, FARTHEST), kl);   // (y.s = 0: all infinitely far, to any reference)
+    y.raise(to);
+  }
   template <bool FULL, int N>
   __device__ __forceinline__ void add(const float (&f)[N], const float (&g)[N]) {
-    float e[N];
+    float dx[N], ex[N];
     const float top = max_of(f);
-    if (x.above(top)) {
-      const float by = x.raise(top);
-      if (FULL) kl *= by;
-    }
-    x.add(f, e);
+    if (x.above(top)) raise_x<FULL>(top);
     if (FULL) {
       const float top_y = max_of(g);
-      if (y.above(top_y)) y.raise(top_y);
+      if (y.above(top_y)) raise_y(top_y);
+    }
+    x.add(f, dx, ex);
+    if (FULL) {
+      float dy[N], ey[N];
+      y.add(g, dy, ey);
 #pragma unroll
-      for (int k = 0; k < N; k++) kl = fmaf(e[k], apart(f[k], g[k]), kl);
-      y.add(g, e);
+      for (int k = 0; k < N; k++) kl = fmaf(ex[k], apart(dx[k], dy[k]), kl);
     }
   }
   template <bool FULL, int LANES>
   __device__ __forceinline__ void over_lanes() {
-    const float by = x.over_lanes<LANES>();
+    raise_x<FULL>(lanes_max<LANES>(x.m));
+    if (FULL) raise_y(lanes_max<LANES>(y.m));
+    x.sum_lanes<LANES>();
     if (FULL) {
-      kl = lanes_sum<LANES>(kl * by);
-      y.over_lanes<LANES>();
+      y.sum_lanes<LANES>();
+      kl = lanes_sum<LANES>(kl);
     }
   }
 };
@@ -293,10 +306,10 @@ __device__ __forceinline__ RowStat row_stat(const Run& others, float xa) {
   return o;
 }
 
-// what the threads of a row need for its gradient: cf exp(x - m), with the exact divergence (cf + ck ((x - y) - kk)) times that, and `own` for the label.  All zeros: a
+// what the threads of a row need for its gradient: cf exp(x - m), with the exact divergence (cf + ck ((x - m) - (y - my))) times that, and `own` for the label.  All zeros: a
 // gradient of zeros.
 struct RowGrad {
-  float m, cf, ck, kk, own;
+  float m, cf, ck, my, own;
 };
 
 // Adds a row to the sums (loss, surrogate, divergence, clipped) and says what its gradient is made of
@@ -318,18 +331,22 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& p, const RowStat& s
   o.cf = (float)(-w * g * s.inv_s);
   o.own = (float)(w * g * (s.rest * s.inv_s));
 }
-// the exact divergence on top; log_ratio: log sum exp x - log sum exp y, NaN where the reference has no distribution: then the divergence is, and with it every element of the gradient
-// (the differences alone do not show it: what is not a number among them counts for something finite)
-__device__ __forceinline__ void full_kl(const PolicyArgs& p, const RowStat& s, double sum_apart, double log_ratio, double* sum, float xa, float ya, double w, RowGrad& o) {
+// The exact divergence on top: the mean distance between the rows less the difference of their logarithms of sums.  NaN where the reference has no distribution, and with it every element
+// of the gradient (the distances alone do not show it: what is not a number among them counts for something finite).
+__device__ __forceinline__ void full_kl(const PolicyArgs& p, const RowStat& s, const RunPair& run, double* sum, float xa, float ya, double w, RowGrad& o) {
   if (s.none) return;
-  const double mine = (double)apart(xa, ya), kk = (sum_apart + (s.ea == 0 ? 0.0 : s.ea * mine)) * s.inv_s;
-  const double kl = kk - log_ratio, nan = kl - kl;   // (0 otherwise)
+  const double x_up = (double)s.m - (double)run.x.m, sum_apart = s.by * ((double)run.kl - (double)run.x.s * x_up);   // (the label may have become the reference)
+  const double mine = fmin(fmax(((double)xa - (double)s.m) - ((double)ya - (double)run.y.m), (double)-FARTHEST), (double)FARTHEST);
+  const double kk = (sum_apart + (s.ea == 0 ? 0.0 : s.ea * mine)) * s.inv_s;
+  const double kl = run.y.s == 0.f ? NAN : kk - (log_d(s.s) - log_d((double)run.y.s)), nan = kl - kl;   // (0 otherwise)
   sum[2] += w * kl;
   if (p.kl_coef == 0) return;
   sum[0] += w * p.kl_coef * kl;
-  o.kk = (float)(kk + nan);
-  o.ck = (float)(w * p.kl_coef * s.inv_s);
-  o.own = (float)((double)o.own + nan + (s.ea != 0 ? w * p.kl_coef * (s.ea * s.inv_s) * (mine - kk) : 0.0));
+  const double ck = w * p.kl_coef * s.inv_s;
+  o.my = run.y.m;
+  o.ck = (float)ck;
+  o.cf = (float)((double)o.cf - ck * kk + nan);
+  o.own = (float)((double)o.own + nan + (s.ea != 0 ? ck * s.ea * (mine - kk) : 0.0));
 }
 
 constexpr int AUX_NT = 2;   // cache policy of a buffer load: non-temporal
@@ -440,8 +457,7 @@ __device__ __forceinline__ RowStat row_result(const PolicyArgs& p, const RunPair
   const RowStat s = row_stat(run.x, in.xa);
   b.m = s.m;
   if (MODE != STATS) policy_row(p, s, sum, in.old, in.adv, in.ref, in.w, b);
-  if (MODE == POLICY_FULL)
-    full_kl(p, s, (double)run.kl * s.by, run.y.s == 0.f ? NAN : ((double)s.m - (double)run.y.m) + (log_d(s.s) - log_d((double)run.y.s)), sum, in.xa, in.ya, in.w, b);
+  if (MODE == POLICY_FULL) full_kl(p, s, run, sum, in.xa, in.ya, in.w, b);
   return s;
 }
 template <Mode MODE>
@@ -492,8 +508,8 @@ template <bool FULL, int N>
 __device__ __forceinline__ void gradient(const RowGrad& b, const float (&f)[N], const float (&g)[N], float (&out)[N]) {
 #pragma unroll
   for (int k = 0; k < N; k++) {
-    const float e = exp_of(f[k] - b.m);
-    out[k] = e * (FULL ? fmaf(b.ck, apart(f[k], g[k]) - b.kk, b.cf) : b.cf);
+    const float d = f[k] - b.m, e = exp_of(d);
+    out[k] = e * (FULL ? fmaf(b.ck, apart(d, g[k] - b.my), b.cf) : b.cf);
   }
 }
 
@@ -715,7 +731,7 @@ __global__ __launch_bounds__(256, 4) void group_kernel(RowArgs a, PolicyArgs p, 
     for (int i = 0; i < ROWS; i++) {
       if (r0 + i >= a.rows) break;
       auto of = [&](float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), i)); };
-      const RowGrad c = {of(b.m), of(b.cf), of(b.ck), of(b.kk), of(b.own)};
+      const RowGrad c = {of(b.m), of(b.cf), of(b.ck), of(b.my), of(b.own)};
       const RowShape<T, 1> s(a.classes, (const T*)a.logits + (long long)(r0 + i) * a.ld, lane);
       const LabelAt place(s, at[i]);
       G* const out = (G*)a.grad + (long long)(r0 + i) * a.gld;

@@ -98,3 +98,39 @@ def test_a_reference_without_a_distribution_where_the_coefficient_is_zero(monkey
     size = (1 + np.abs(w["logp"])) * np.abs(c.adv) * (1 + np.exp(w["logp"] - c.old)) / 6
     close(c.loss.item(), w["loss"], R * size.sum(), "loss")
     close(c.grad.host(), w["grad"], half_step(False) * np.abs(w["grad"]) + R * size[:, None] + 1e-37, "grad")
+
+
+@pytest.mark.parametrize("rows,C,bf16,kw", REFERENCES)
+def test_rows_of_the_lowest_value_on_one_side(rows, C, bf16, kw):
+    """Nothing but the type's lowest value is an even distribution, also where the other side's logits are ordinary ones."""
+    def edit(c):
+        c.label[:5] = 3
+        c.x[1], c.y[2] = LOWEST[bf16], LOWEST[bf16]
+        c.y[3, 50:] = c.x[3, 50:] = LOWEST[bf16]
+        c.x[4] = np.where(np.arange(C) % 2, c.x[4], LOWEST[bf16])
+        c.old[:5] = -np.log(C)
+
+    c = Policy(rows, C, bf16, "full", edit=edit, masked=0.1 if rows > 6 else 0, **kw).call()
+    w = c.want()
+    bound, each = _shifted(c, w)
+    assert w["stats"][1] < 100
+    close(c.loss.item(), w["loss"], each.sum(), "loss")
+    close(c.stats.cpu().numpy()[:2], w["stats"][:2], each.sum() / KL, "stats")
+    if c.grad:
+        close(c.grad.host(), w["grad"], bound, "grad")
+
+
+@pytest.mark.parametrize("by", [3e4, 1e7, -1e7, 1e30])
+@pytest.mark.parametrize("rows,C,train", [(5, 200, True), (5, 6000, True), (5, 70001, True), (4500, 40, True), (5, 40001, False)])
+def test_a_shift_between_policy_and_reference(rows, C, train, by):
+    """Logits count up to a constant per row: what both rows have in common does not reach the divergence."""
+    def edit(c):
+        c.y = np.float32(c.y + by).astype(np.float64)
+
+    c = Policy(rows, C, False, "full", edit=edit, train=train, masked=0).call()
+    w = c.want()
+    bound, each = _shifted(c, w)
+    close(c.loss.item(), w["loss"], each.sum(), "loss")
+    close(c.stats[1].item(), w["stats"][1], each.sum() / KL, "divergence")
+    if train:
+        close(c.grad.host(), w["grad"], bound, "grad")
