@@ -162,37 +162,31 @@ __device__ __forceinline__ float lanes_sum(float v) {
 }
 
 // ---- softmax statistics as they run along a row.  m: the reference, at first the maximum of what came first and raised only to what lies far above it (sums of
-// numbers up to 2^16 are as exact as those of numbers up to 1); s = sum exp(x - m); of the first element of each vector, s0 = sum exp(x - m) and t = sum exp(x - m) (x - m).
-struct Run {
-  float m, s, s0, t;
-  __device__ __forceinline__ void start() { m = LOWEST, s = s0 = t = 0.f; }
+// numbers up to 2^16 are as exact as those of numbers up to 1); s = sum exp(x - m).
+struct Sum {
+  float m, s;
+  __device__ __forceinline__ void start() { m = LOWEST, s = 0.f; }
+  __device__ __forceinline__ bool above(float top) const { return top > m + 11.f; }
   __device__ __forceinline__ float raise(float to) {   // returns the factor
     const float f = exp_of(m - to);
-    t = f * fmaf(s0, fmaxf(m - to, -1e4f), t);
     m = to;
     s *= f;
+    return f;
+  }
+};
+// and of the first element of each vector, s0 = sum exp(x - m) and t = sum exp(x - m) (x - m)
+struct Run : Sum {
+  float s0, t;
+  __device__ __forceinline__ void start() { Sum::start(), s0 = t = 0.f; }
+  __device__ __forceinline__ float raise(float to) {
+    const float by = fmaxf(m - to, -1e4f), f = Sum::raise(to);   // (beyond 1e4 nothing is left of the terms)
+    t = f * fmaf(s0, by, t);
     s0 *= f;
     return f;
   }
-  __device__ __forceinline__ bool above(float top) const { return top > m + 11.f; }
-  template <int N>
-  __device__ __forceinline__ void add(const float (&f)[N], float (&d)[N], float (&e)[N]) {   // d: the distances to m, e: the terms
-#pragma unroll
-    for (int k = 0; k < N; k++) d[k] = f[k] - m;
-#pragma unroll
-    for (int k = 0; k < N; k++) e[k] = exp_of(d[k]);
-    t = fmaf(e[0], fmaxf(d[0], -1e4f), t);
-    s0 += e[0];
-    float a = e[0];
-#pragma unroll
-    for (int k = 1; k < N; k++) a += e[k];
-    s += a;
-  }
-  template <int LANES>
-  __device__ __forceinline__ void sum_lanes() {   // of one m
-    s = lanes_sum<LANES>(s);
-    s0 = lanes_sum<LANES>(s0);
-    t = lanes_sum<LANES>(t);
+  __device__ __forceinline__ void first(float d, float e) {
+    t = fmaf(e, fmaxf(d, -1e4f), t);
+    s0 += e;
   }
 };
 // (the builtin maximum would first quiet every operand, an instruction each)
@@ -214,13 +208,14 @@ constexpr float FARTHEST = 1e30f;
 __device__ __forceinline__ float apart(float dx, float dy) { return __builtin_amdgcn_fmed3f(dx - dy, -FARTHEST, FARTHEST); }
 // Two rows at once, and kl = sum over x's terms of term * (dx - dy): of distances, so that what a whole row has in common, be it the type's lowest value, does not count
 struct RunPair {
-  Run x, y;
+  Run x;
+  Sum y;
   float kl;
   __device__ __forceinline__ void start() { x.start(), y.start(), kl = 0.f; }
   template <bool FULL>
   __device__ __forceinline__ void raise_x(float to) {
-    const float by = fminf(to - x.m, 1e4f), s = x.s, f = x.raise(to);   // (beyond 1e4 nothing is left of the terms)
-    if (FULL) kl = f * fmaf(-s, by, kl);
+    const float by = fmaxf(x.m - to, -1e4f), s = x.s, f = x.raise(to);
+    if (FULL) kl = f * fmaf(s, by, kl);
   }
   __device__ __forceinline__ void raise_y(float to) {
     if (y.s != 0.f) kl = fmaf(x.s, fminf(to - y.m, FARTHEST), kl);   // (y.s = 0: all infinitely far, to any reference)
@@ -228,28 +223,36 @@ struct RunPair {
   }
   template <bool FULL, int N>
   __device__ __forceinline__ void add(const float (&f)[N], const float (&g)[N]) {
-    float dx[N], ex[N];
     const float top = max_of(f);
     if (x.above(top)) raise_x<FULL>(top);
     if (FULL) {
       const float top_y = max_of(g);
       if (y.above(top_y)) raise_y(top_y);
     }
-    x.add(f, dx, ex);
-    if (FULL) {
-      float dy[N], ey[N];
-      y.add(g, dy, ey);
+    float sx = 0.f, sy = 0.f;
 #pragma unroll
-      for (int k = 0; k < N; k++) kl = fmaf(ex[k], apart(dx[k], dy[k]), kl);
+    for (int k = 0; k < N; k++) {
+      const float dx = f[k] - x.m, ex = exp_of(dx);
+      if (k == 0) x.first(dx, ex);
+      sx = k == 0 ? ex : sx + ex;
+      if (FULL) {
+        const float dy = g[k] - y.m, ey = exp_of(dy);
+        kl = fmaf(ex, apart(dx, dy), kl);
+        sy = k == 0 ? ey : sy + ey;
+      }
     }
+    x.s += sx;
+    if (FULL) y.s += sy;
   }
   template <bool FULL, int LANES>
   __device__ __forceinline__ void over_lanes() {
     raise_x<FULL>(lanes_max<LANES>(x.m));
     if (FULL) raise_y(lanes_max<LANES>(y.m));
-    x.sum_lanes<LANES>();
+    x.s = lanes_sum<LANES>(x.s);
+    x.s0 = lanes_sum<LANES>(x.s0);
+    x.t = lanes_sum<LANES>(x.t);
     if (FULL) {
-      y.sum_lanes<LANES>();
+      y.s = lanes_sum<LANES>(y.s);
       kl = lanes_sum<LANES>(kl);
     }
   }
@@ -335,8 +338,8 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& p, const RowStat& s
 // of the gradient (the distances alone do not show it: what is not a number among them counts for something finite).
 __device__ __forceinline__ void full_kl(const PolicyArgs& p, const RowStat& s, const RunPair& run, double* sum, float xa, float ya, double w, RowGrad& o) {
   if (s.none) return;
-  const double x_up = (double)s.m - (double)run.x.m, sum_apart = s.by * ((double)run.kl - (double)run.x.s * x_up);   // (the label may have become the reference)
-  const double mine = fmin(fmax(((double)xa - (double)s.m) - ((double)ya - (double)run.y.m), (double)-FARTHEST), (double)FARTHEST);
+  const double sum_apart = s.by * (double)fmaf(run.x.s, fmaxf(run.x.m - s.m, -1e4f), run.kl);   // (the label may have become the reference)
+  const double mine = (double)apart(xa - s.m, ya - run.y.m);
   const double kk = (sum_apart + (s.ea == 0 ? 0.0 : s.ea * mine)) * s.inv_s;
   const double kl = run.y.s == 0.f ? NAN : kk - (log_d(s.s) - log_d((double)run.y.s)), nan = kl - kl;   // (0 otherwise)
   sum[2] += w * kl;
