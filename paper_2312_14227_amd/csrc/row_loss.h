@@ -300,7 +300,7 @@ __device__ __forceinline__ RowStat row_stat(const Run& others, float xa) {
   o.m = above ? xa : others.m;
   o.by = above ? e : 1.0;
   o.ea = above ? 1.0 : e;
-  o.rest = (double)others.s * o.by;
+  o.rest = u == INFINITY ? NAN : (double)others.s * o.by;   // (an infinite logit has no log probability: infinity less infinity)
   o.s = o.rest + o.ea;
   o.inv_s = 1.0 / o.s;
   o.none = o.s == 0.0;

@@ -134,3 +134,29 @@ def test_a_shift_between_policy_and_reference(rows, C, train, by):
     close(c.stats[1].item(), w["stats"][1], each.sum() / KL, "divergence")
     if train:
         close(c.grad.host(), w["grad"], bound, "grad")
+
+
+@pytest.mark.parametrize("kl", ["none", "sampled", "full"])
+@pytest.mark.parametrize("rows,C,bf16,kw", [(6, 200, False, {}), (6, 6000, True, {}), (6, 140001, True, {}), (4500, 40, True, {}), (6, 5001, True, dict(in_place=True))])
+def test_an_infinite_logit_of_the_label(rows, C, bf16, kw, kl):
+    """Infinity less infinity, as with any other class of infinite logit: NaN, in its row alone."""
+    def edit(c):
+        c.label[:3] = 1
+        c.x[1, 1] = np.inf
+
+    c = Policy(rows, C, bf16, kl, edit=edit, masked=0, **kw).call()
+    g = c.grad.host()
+    assert np.isnan(c.loss.item()) and np.isnan(c.logp[1].item()) and np.isnan(g[1]).all() and np.isfinite(np.delete(g, 1, 0)).all()
+
+
+@pytest.mark.parametrize("lengths,C,bf16,offsets", [([1, 1, 1, 1], 300, True, False), ([1, 1, 1, 1], 300, True, True), ([1, 1, 1, 1], 9000, False, False), ([3, 2, 1, 4], 60001, True, True),
+                                                    ([1500, 1500, 900, 900], 100, True, True)])
+def test_an_infinite_logit_of_the_label_of_a_pair(lengths, C, bf16, offsets):
+    def edit(c):
+        c.label[:] = 1
+        c.x[0, 1] = np.inf
+
+    c = Preference(lengths, C, bf16, edit=edit, masked=0, ref=False, offsets=offsets, beta=0.01).call()
+    n = lengths[0] + lengths[1]
+    g = c.grad.host()
+    assert np.isnan(c.loss.item()) and np.isnan(c.logp[0].item()) and np.isnan(g[:n]).all() and np.isfinite(g[n:]).all()
