@@ -326,8 +326,8 @@ int et_policy_loss(int32_t rows, int32_t classes, const void* logits_dev, int32_
  * one of pair p, 2p + 1 the other.  With L[i] the sum of its unmasked rows' log probabilities of their labels (0 of an empty sequence):
  *   z = beta * ((L[2p] - ref[2p]) - (L[2p+1] - ref[2p+1]))
  *   loss = mean over pairs of -(1 - label_smoothing) log sigmoid(z) - label_smoothing log sigmoid(-z)
- * At most 2^23 pairs.  Rows in front of the first sequence and behind the last are neither read nor written.  Offsets that descend or leave [0, rows]
- * are cut to where they do not. */
+ * At most 2^23 pairs.  Rows in front of the first sequence and behind the last are neither read nor written, and count for nothing.  Offsets that leave [0, rows] are cut to it.
+ * Where they descend, a sequence that ends in front of its beginning is empty, a row in several sequences counts in each, and the gradient is zero. */
 typedef struct {
   const int32_t* offsets_dev;   /* [2 pairs + 1], ascending; NULL: every row is a sequence (rows = 2 pairs) */
   const float* ref_logp_dev;    /* [2 pairs] the reference's sums; NULL: zeros */

@@ -285,6 +285,11 @@ struct SeqRows {   // per row, in the workspace
   double* lp;
   float *m, *s, *rest;   // (s = 0: masked, or without a distribution)
   float* g;              // the gradient is g ([j = a] - p[j])
+  int* descend;          // of all: whether offsets descend, so that a row may be in several sequences
+  // (the statistics' launch clears it for that of the pairs)
+  __device__ __forceinline__ void clear() const {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *descend = 0;
+  }
 };
 
 // what a row's statistics come to: s = sum of the terms against m, ea the label's, rest the others', by: what others' terms were multiplied with
@@ -532,6 +537,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 4) void kept_kernel(RowArgs 
   __shared__ int red_n[16];
   const int t = threadIdx.x % TPR, team = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   const int step = gridDim.x * TEAMS;
+  if (MODE == STATS) o.clear();
   const int begin = MODE == STATS ? seq.at(0) : 0, end = MODE == STATS ? seq.at(seq.n) : a.rows;
   auto label_of = [&](int r) {
     const int label = a.label[r];
@@ -665,6 +671,7 @@ __global__ __launch_bounds__(256, 4) void group_kernel(RowArgs a, PolicyArgs p, 
   __shared__ double sums[4][COLUMNS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   double unit = 0, sum[4] = {0, 0, 0, 0}, seen = 0;
+  if (MODE == STATS) o.clear();
   if (MODE != STATS && !p.weight) unit = GRAD ? unit_weight(a, counts, n_counts, red_n) : 1.0;
   const int begin = MODE == STATS ? seq.at(0) : 0, end = MODE == STATS ? seq.at(seq.n) : a.rows;
   for (long long first = (long long)wave * ROWS; first < a.rows; first += (long long)gridDim.x * 4 * ROWS) {
@@ -785,6 +792,7 @@ __global__ __launch_bounds__(64 * W, 4) void streamed_kernel(RowArgs a, PolicyAr
   __shared__ int red_n[16];
   const int t = threadIdx.x;
   double unit = 0;
+  if (MODE == STATS) o.clear();
   if (MODE != STATS) {
     if (threadIdx.x < COLUMNS) sums[threadIdx.x] = 0;
     if (!p.weight) unit = GRAD ? unit_weight(a, counts, n_counts, red_n) : 1.0;

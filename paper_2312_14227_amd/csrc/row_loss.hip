@@ -175,12 +175,13 @@ __global__ __launch_bounds__(256) void pair_rows_kernel(RowArgs a, PairArgs q, d
   }
 }
 
-// A workgroup a pair, a half of it a sequence: the sums of its rows, eight a thread at once, then the rows' factors
+// A workgroup a pair, a half of it a sequence: the sums of its rows, eight a thread at once, then the rows' factors.  Where offsets descend several workgroups may write a row's: then none is used
 __global__ __launch_bounds__(256) void pair_kernel(Sequences seq, SeqRows o, PairArgs q, double* __restrict__ parts) {
   constexpr int AT_ONCE = 8;
   __shared__ double red[4];
   const int pair = blockIdx.x, i = threadIdx.x >> 7, t = threadIdx.x & 127;
   const int begin = seq.at(2 * pair + i), end = seq.at(2 * pair + i + 1);
+  if (t == 0 && end < begin) atomicOr(o.descend, 1);
   double v = 0;
   for (int r0 = begin + t; r0 < end; r0 += AT_ONCE * 128) {
     double lp[AT_ONCE];
@@ -216,6 +217,7 @@ __global__ __launch_bounds__(256) void pair_grad_kernel(RowArgs a, Sequences seq
   constexpr int N = Vec<T>::N, PIECE = 64 * N * GRAD_VECS;
   const int begin = seq.at(0), end = seq.at(seq.n), lane = threadIdx.x & 63;
   const int C = a.classes, Cv = C - C % N, pieces = (C - 1) / PIECE + 1;
+  const bool descend = *o.descend != 0;
   const long long tasks = (long long)(end - begin) * pieces;
   for (long long task = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); task < tasks; task += (gridDim.x - 1) * 4ll) {
     const int r = begin + (int)(task / pieces), j0 = (int)(task % pieces) * PIECE;
@@ -223,7 +225,7 @@ __global__ __launch_bounds__(256) void pair_grad_kernel(RowArgs a, Sequences seq
     const T* x = (const T*)a.logits + (long long)r * a.ld;
     const int at = a.label[r];
     const float s = o.s[r], m = o.m[r], g = o.g[r];
-    const bool zero = s == 0.f;
+    const bool zero = s == 0.f || descend;
     const float cf = zero ? 0.f : -g / s, own = zero ? 0.f : g * (o.rest[r] / s);
     auto one = [&](float f, int j) { return zero ? 0.f : j == at ? own : cf * exp_of(f - m); };
     u32x4 v[GRAD_VECS];
@@ -361,6 +363,7 @@ int et_op::preference_loss(int32_t rows, int32_t pairs, int32_t classes, const v
   c.o.s = c.o.m + rows;
   c.o.rest = c.o.s + rows;
   c.o.g = c.o.rest + rows;
+  c.o.descend = (int*)(c.o.g + rows);
   const et::rows::RowPlan plan = et::rows::row_plan(rows, classes, type_size(dtype), false, false, grad_dev != nullptr, device_cus(on.dev));
   const int grid = plan.waves == 1 ? et::rows::row_grid(rows, plan) : std::min(rows, 1 << 20);
   if (dtype == ET_BF16) et::rows::rows_of_statistics<bf16>(plan, grid, s, c);

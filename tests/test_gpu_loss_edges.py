@@ -160,3 +160,33 @@ def test_an_infinite_logit_of_the_label_of_a_pair(lengths, C, bf16, offsets):
     n = lengths[0] + lengths[1]
     g = c.grad.host()
     assert np.isnan(c.loss.item()) and np.isnan(c.logp[0].item()) and np.isnan(g[:n]).all() and np.isfinite(g[n:]).all()
+
+
+@pytest.mark.parametrize("C,bf16", [(40, False), (130, True), (9001, True), (140001, True)])
+@pytest.mark.parametrize("offsets", [[0, 5, 3, 8, 10], [5, 3, 9, -7, 100], [0, 10, 0, 10, 10], [10, 4, 6, 2, 0], [2, 9, 9, 1, 8], [-2 ** 31, 7, 2 ** 31 - 1, 3, 9], [3, 8, 2, 2, 2]])
+def test_offsets_that_descend(offsets, C, bf16):
+    """A row in several sequences counts in each, one that ends in front of its beginning is empty, and the gradient is zero: the same bits every time."""
+    import torch
+    from loss_util import dev
+    c = Preference([3, 2, 4, 1], C, bf16, masked=0.1, ref=False, beta=0.5)
+    c.d[1] = dev(offsets, np.int32)
+    c.call()
+    o, R = np.clip(offsets, 0, c.rows), 4 * rel(C)
+    L, size = np.zeros(4), np.zeros(4)
+    for i in range(4):
+        for r in range(max(o[i], o[0]), min(o[i + 1], o[4])):
+            if 0 <= c.label[r] < C:
+                lp = losses.log_softmax(c.x[r])[c.label[r]]
+                L[i], size[i] = L[i] + lp, size[i] + 1 + abs(lp)
+    z = c.beta * (L[0::2] - L[1::2])
+    off = R * c.beta * (size[0::2] + size[1::2]) + 2.0 ** -23 * np.abs(z)
+    close(c.logp.cpu().numpy(), L, R * size + 2.0 ** -24 * np.abs(L), "logp")
+    close(c.loss.item(), np.logaddexp(0, -z).mean(), off.mean() + R, "loss")
+    close(c.stats[0].item(), z.mean(), off.mean(), "margin")
+    g = c.grad.host()
+    assert (g[o[0]:max(o[0], o[4])] == 0).all() and (np.delete(g, range(o[0], max(o[0], o[4])), 0) == c.grad.fill).all() and c.grad.untouched()
+    first = [t.clone() for t in c.outputs()]
+    c.call(stream=torch.cuda.Stream())
+    assert all(torch.equal(a, b) for a, b in zip(first, c.outputs()))
+    c.d[1] = dev(c.offsets, np.int32)                            # and nothing of it is left for the next call
+    c.call().check()
