@@ -37,12 +37,18 @@ inline int device_cus(int dev) {
   return hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0 ? n : 256;
 }
 
-// bytes [begin, end) of a matrix of `rows` rows
+// A matrix of `rows` rows: bytes from the first to behind the last, of a row, from a row to the next
 struct Span {
-  uintptr_t begin, end;
+  uintptr_t begin, end, width, step;
   Span(const void* p, int64_t rows, int64_t cols, int64_t stride, size_t size)
-      : begin(reinterpret_cast<uintptr_t>(p)), end(begin + (size_t)((rows - 1) * stride + cols) * size) {}
-  bool meets(const Span& o) const { return begin < o.end && o.begin < end; }
+      : begin(reinterpret_cast<uintptr_t>(p)), end(begin + (size_t)((rows - 1) * stride + cols) * size), width((size_t)cols * size), step((size_t)stride * size) {}
+  // Whether two have a byte in common, if they are as many bytes from row to row apart: rows may lie beside each other's.  Otherwise whether what they reach over does
+  bool meets(const Span& o) const {
+    if (begin >= o.end || o.begin >= end) return false;
+    if (step != o.step || step == 0) return true;
+    const uintptr_t at = o.begin >= begin ? (o.begin - begin) % step : (step - (begin - o.begin) % step) % step;   // where o's rows begin, counted from the beginning of these
+    return at < width || at + o.width > step;
+  }
 };
 
 // The losses, without and with their launches (row_loss.hip); launches: how many (nullable)
