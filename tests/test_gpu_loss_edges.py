@@ -202,20 +202,25 @@ def _together(bf16, rows, C, parts, pad):
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("C,pad", [(200, 0), (1001, 3), (33001, 0)])
 def test_matrices_whose_rows_lie_beside_each_other(C, pad, bf16):
-    """Logits, the reference's and the gradient in one buffer, and the gradient in the logits' place beside the reference: as in buffers of their own."""
+    """Logits, the reference's and the gradient in one buffer, and the gradient in the logits' place beside the reference: within the bounds of the definition.  (Not the bits of
+    buffers of their own: the vectors of a row begin at multiples of 16 bytes, so its address decides in which order its C terms are added, and two orders of them differ by up to
+    2 (C / 64 + 20) roundings of 2^-24, of which the bound counts as many for each.)"""
     import torch
     from paper_2312_14227_amd import binding as et
-    c = Policy(7, C, bf16, "full", masked=0.2).call()
-    want, ty = [t.clone() for t in (c.grad.view, c.loss, c.logp)], et.ET_BF16 if bf16 else et.ET_F32
+    c = Policy(7, C, bf16, "full", masked=0.2).call().check()
+    ty = et.ET_BF16 if bf16 else et.ET_F32
     for in_place in (False, True):
         flat, part = _together(bf16, 7, C, 3, pad)
         part[0].copy_(c.logits.view), part[1].copy_(c.refs.view)
         grad, stride = part[0 if in_place else 2], flat.shape[1]
         p = et.make_policy(c.d["old"].data_ptr(), c.d["adv"].data_ptr(), ref_logits=part[1].data_ptr(), ref_stride=stride, clip_low=c.p.clip_low, clip_high=c.p.clip_high,
-                           kl_coef=KL, logp=c.logp.data_ptr())
+                           kl_coef=KL, logp=c.logp.data_ptr(), stats=c.stats.data_ptr())
+        for t in (c.loss, c.logp, c.stats, c.grad.view):
+            t.fill_(7.0)
         et.et_policy_loss(7, C, part[0].data_ptr(), ty, stride, c.d["label"].data_ptr(), p, grad.data_ptr(), ty, stride, c.ws.data_ptr(), c.ws.numel(),
                           torch.cuda.current_stream().cuda_stream, c.loss.data_ptr())
         torch.cuda.synchronize()
-        assert all(torch.equal(a, b) for a, b in zip(want, (grad, c.loss, c.logp)))
+        c.grad.put(grad)
+        c.check()
         assert torch.equal(part[1], c.refs.view) and (in_place or torch.equal(part[0], c.logits.view))
         assert bool((flat[:, [k * (C + pad) + C + i for k in range(3) for i in range(pad)]] == -3.0).all())
