@@ -278,7 +278,7 @@ int et_train_step(et_ctx* ctx, const void* x_dev, const int32_t* y_dev, const ui
 
 /* ---- Losses of log probabilities, and what is done to many gradients at once: stand-alone operators.
  * Like et_importance_reduce_static they take device pointers and host descriptors that are read before the call returns,
- * enqueue a few kernels on `hip_stream` (NULL = the default stream of the current device) on that stream's device, allocate nothing,
+ * enqueue a few kernels on `hip_stream` (NULL = the default stream of the current device) on that stream's device, allocate no device memory,
  * copy nothing from or to host memory and do not wait, so that a call may be captured into a graph.  Their scratch is
  * `workspace_dev`: 16-byte aligned, at least the bytes that the function beside each states (which depend on the sizes alone), in
  * any state; a call leaves nothing in it that a later one reads.  Calls (and replays of captured ones) that share a workspace must not overlap.
@@ -291,7 +291,8 @@ int et_train_step(et_ctx* ctx, const void* x_dev, const int32_t* y_dev, const ui
  * (same stride and type), and must not overlap the logits otherwise (ET_EINVAL); rows of matrices of one stride in bytes may lie beside each other in one buffer.  Pointers need their element's alignment only.  Elements between the rows are
  * neither read nor written.  label_dev[r] is the row's class (the action taken, the token produced); one outside [0, classes) masks the
  * row: its logits and its other inputs are not used, whatever they hold, and its gradient is zero.  A logit of minus infinity has
- * probability zero and gradient zero; a row with nothing but those has no distribution: it gives no loss and a gradient of zero, but counts among the unmasked.
+ * probability zero and gradient zero; a row with nothing but those has no distribution: it gives no loss and a gradient of zero, but counts among the unmasked.  NaN or plus infinity among
+ * an unmasked row's logits makes its log probability, its gradient and the loss NaN.
  * Softmax statistics are held in float32, a row's log probability and everything that is derived from it per row, and the sums over rows in float64;
  * gradients are rounded once. */
 
@@ -300,10 +301,13 @@ int et_train_step(et_ctx* ctx, const void* x_dev, const int32_t* y_dev, const ui
  *   clipped   = (A > 0 and ratio > 1 + clip_high) or (A < 0 and ratio < 1 - clip_low)
  *   surrogate = A * (clipped ? that border : ratio)        (the smaller of the clipped and the unclipped product)
  *   kl        = exp(d) - d - 1, d = ref_logp - lp          if ref_logp_dev is given: an estimate from the label alone, never negative
- *             = sum_j p[j] (log p[j] - log q[j])           if ref_logits_dev is: exactly, q their softmax
+ *             = sum_j p[j] (log p[j] - log q[j])           if ref_logits_dev is: over all classes, q their softmax
  *             = 0                                          if neither is (both: ET_EINVAL)
  *   loss      = sum over unmasked rows of weight * (kl_coef * kl - surrogate);  weight_dev == NULL: 1 / (number of unmasked rows)
  * The gradient is that of `loss`; old_logp, advantage, the reference and the weights are constants, and a clipped row's surrogate has none.
+ * Over all classes, a class may lie at most 1e30 further below its row's largest logit in one row than in the other: more, and minus infinity in the reference alone, where the divergence is infinite,
+ * counts as 1e30.  So kl is finite there, at least about 1e30 p[j]; look for large values, not for infinite ones.  A class at minus infinity in both, or in the logits alone, counts for nothing.
+ * Reference logits with NaN or plus infinity among them, or of nothing but minus infinity, are no distribution: kl, the row's gradient and the loss are NaN (kl alone if kl_coef is 0).
  * No unmasked row: loss 0. */
 typedef struct {
   const float* old_logp_dev;    /* [rows] log probability of the label when it was drawn */

@@ -203,7 +203,9 @@ struct Plan {
 
 // The chunk from which on the norm reads through the caches: what follows a norm, clipping or an update, reads the same gradients, and finds the last 192 MB in the last-level
 // cache (256 MB).  86 million float32 gradients: norm and scaling 169 us, past the caches 185.  Up to 128 MB are read past the caches all the same (60 million bf16:
-// 24 us, through them 26), as is what lies in front of the last 192 MB of more (303 million float32: 188 and 208).
+// 24 us, through them 26), as is what lies in front of the last 192 MB of more (303 million float32: 188 and 208).  That is the norm's side of it.  With the scaling that follows, calls of
+// up to 128 MB would gain through the caches (float32 into other outputs: 10 million 24.5 us instead of 29.5, 30 million 65.6 instead of 72.2; 30 million in place 77.7 instead of 80.3), and calls
+// that find nothing to scale would lose (2.5 million 10.5 instead of 9.7, 30 million 28.8 instead of 25.8).
 uint32_t cached_from(const Plan& p, size_t size) {
   const double bytes = (double)p.total * size;
   if (bytes <= 128e6) return UINT32_MAX;

@@ -6,7 +6,8 @@
 //
 // What bounds them: memory, with the vector units close behind.  An element costs a row's statistics some 8 issue slots, four of them the exponential, and the
 // gradient 8 more: by count, a row of 128000 bf16 classes takes a compute unit 18 us of those and 24 us of its share of the memory.  Policy loss with gradient of 8192 such rows:
-// 813 us, 5.2 TB/s; its value alone of 2048 rows of 32000, one in five masked: 25.4 us, 4.1 TB/s; exact divergence of 4096 rows of 50257, one in ten masked: 263 us, 4.4 TB/s.
+// 813 us, 5.2 TB/s; its value alone of 2048 rows of 32000, one in five masked: 25.4 us, 4.1 TB/s; exact divergence of 4096 rows of 50257, one in ten masked: 263 us, 4.4 TB/s (calls that
+// go on; the first thirty of a process take up to 306).
 #pragma once
 #include <cmath>
 #include <type_traits>
@@ -388,9 +389,10 @@ __device__ __forceinline__ int count_rows(const RowArgs& a, int begin, int end, 
   }
   return block_count(n, red);
 }
-// ---- rows.  Both kernels below go over the rows r = first, first + step, ...; the threads of a row ("team") are t = 0 .. TPR - 1.  Vectors of a row are those that
+// ---- rows.  The kernels below go over the rows r = first, first + step, ...; the threads of a row ("team") are t = 0 .. TPR - 1.  Vectors of a row are those that
 // begin at multiples of 16 bytes: vector v of thread t at element head + (v * TPR + t) * N.  What lies in front of the first and behind the last is one element each of the
-// first threads (loads and stores of vectors at any element are right too, and cost 8192 rows of 100003 bf16 classes 10 per cent, and 24 where they are only read).
+// first threads (loads and stores of vectors at any element are right too, and cost 8192 rows of 100003 bf16 classes 10 per cent, and 24 where they are only read; the second pass of a
+// preference loss makes them).  Of the reference's rows the same elements are loaded as vectors, wherever its rows begin.
 template <typename T, int W>
 struct RowShape {
   static constexpr int N = Vec<T>::N, TPR = 64 * W;

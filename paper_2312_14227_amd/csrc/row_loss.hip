@@ -205,7 +205,8 @@ __global__ __launch_bounds__(256) void pair_kernel(Sequences seq, SeqRows o, Pai
   }
 }
 
-// The gradient once the factors are known: nothing but a map of the logits.  A wave takes GRAD_VECS vectors a lane of a row at a time.  The last workgroup adds up the pairs.
+// The gradient once the factors are known: nothing but a map of the logits.  A wave takes GRAD_VECS vectors a lane of a row at a time, from its first element on,
+// at whatever address that lies.  The last workgroup adds up the pairs.
 constexpr int GRAD_VECS = 8;
 template <typename T, typename G>
 __global__ __launch_bounds__(256) void pair_grad_kernel(RowArgs a, Sequences seq, SeqRows o, const double* __restrict__ parts, float* __restrict__ loss,
