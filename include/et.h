@@ -288,8 +288,8 @@ int et_train_step(et_ctx* ctx, const void* x_dev, const int32_t* y_dev, const ui
  *
  * Logits: row r (of at most 2^30) of `classes` (at most 2^28) values starts at logits_dev + r * row_stride (in elements, row_stride >= classes), of type `dtype` (ET_F32 |
  * ET_BF16).  The gradient has the same shape, a stride and a type of its own; grad_dev == NULL: no gradient is computed.  It may be logits_dev itself
- * (same stride and type), and must not overlap the logits otherwise (ET_EINVAL); rows of matrices of one stride in bytes may lie beside each other in one buffer.  Pointers need their element's alignment only.  Elements between the rows are
- * neither read nor written.  label_dev[r] is the row's class (the action taken, the token produced); one outside [0, classes) masks the
+ * (same stride and type), and must not overlap the logits otherwise (ET_EINVAL); rows of matrices of one stride in bytes may lie beside each other in one buffer.
+ * Pointers need their element's alignment only.  Elements between the rows are neither read nor written.  label_dev[r] is the row's class (the action taken, the token produced); one outside [0, classes) masks the
  * row: its logits and its other inputs are not used, whatever they hold, and its gradient is zero.  A logit of minus infinity has
  * probability zero and gradient zero; a row with nothing but those has no distribution: it gives no loss and a gradient of zero, but counts among the unmasked.  NaN or plus infinity among
  * an unmasked row's logits makes its log probability, its gradient and the loss NaN.
